@@ -283,7 +283,7 @@ def _plain_plan(s):
     pos = torch.where(ok, cached[r] + t - start[r], 0)
     slot = torch.where(ok, table[r, pos // P].long() * P + pos % P, -1)
     pos = torch.where(ok, pos, -1)
-    used = torch.where(fits, first + take, 0).max()
+    used = torch.where(fits & (take > 0), first + take, 0).max()
     i32 = torch.int32
     return dict(table=table, slot=slot.to(i32), pos=pos.to(i32), token_start=torch.cat([start, end[-1:]]).to(i32),
                 kv_len=torch.where(fits, cached + new, cached).to(i32), head=(head + used).to(i32))
@@ -440,7 +440,7 @@ def _exact_plan(case, s):
             for i in range(n):
                 pos[start[-1] + i] = c + i
                 slot[start[-1] + i] = table[r][(c + i) // P] * P + (c + i) % P
-            used = max(used, asked + more)
+            used = asked + more if more else used
         kv_len.append(c + n if room else c)
         asked += more
         start.append(start[-1] + n)
