@@ -444,6 +444,140 @@ sq_status sq_calib_search(const uint16_t* x, int32_t M, const int32_t* tok2strea
                           float* clip_out, double* objective_out, void* workspace, size_t workspace_bytes,
                           hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * A decoder's token step around the int4 linears: what the quantized DiT keeps
+ * in 16 bits (norm, rotation, softmax, KV cache; App. D) as its own kernels.
+ * One step is sq_kv_plan, a qkv linear, sq_qk_norm_rope, sq_attn_paged and an
+ * out linear; with few tokens the linears are sq_linear_w4a16.  Every entry
+ * point follows the conventions at the top of this header.
+ *
+ * The paged cache: K and V each [num_pages][num_heads][page_size][head_dim],
+ * contiguous.  A slot is page * page_size + offset within the page. */
+typedef struct sq_kv_cache {
+  void* k;            /* 16-byte aligned, of dtype */
+  void* v;            /* the same shape and type */
+  int32_t num_pages;  /* >= 1; num_pages * page_size < 2^31 */
+  int32_t num_heads;  /* key-value heads, 1 .. 256 */
+  int32_t page_size;  /* tokens per page: a power of two, 8 .. 1024 */
+  int32_t head_dim;   /* 64, 96, 128, 192 or 256 */
+  int32_t dtype;      /* SQ_OUT_BF16 or SQ_OUT_F16 */
+} sq_kv_cache;
+
+/* Block tables and slot maps from request lengths, on the device: request r
+ * holds cached_len[r] tokens and gets new_len[r] more (negative lengths count
+ * as 0), its pages in table[r][0 .. ceil(cached / page_size)).  With
+ *     take  = ceil((cached + new) / page_size) - ceil(cached / page_size)
+ *             (0 where the request would need more than max_pages)
+ *     first = sum of take, start = sum of new over the requests before r
+ *     head  = *free_head
+ * request r is placed if it needs at most max_pages pages, its pages are there
+ * (take == 0, or head + first + take <= num_free) and its tokens have entries
+ * (start + new <= max_tokens).  For a placed request
+ *     table[r][ceil(cached / page_size) + i] = free_pages[head + first + i], i < take
+ *     pos[start + t] = cached + t,  slot[start + t] = the slot of that position
+ *     kv_len[r] = cached + new
+ * A request that is not placed keeps its table row and kv_len[r] = cached, and
+ * its entries of pos and slot are -1, as are those from the last start on.
+ * *free_head_out = head + the pages taken (first + take of the last placed
+ * request with take > 0): the pages from there on are still free.
+ *   cached_len, new_len  int32 [num_requests], 1 .. 8192 requests
+ *   free_pages           int32 [num_free] (may be NULL when num_free is 0)
+ *   free_head            int32 [1], in [0, num_free] (clamped), or NULL for 0
+ *   table                int32 [num_requests][max_pages], in and out: only
+ *                        entries of newly taken pages are written; those that
+ *                        slots are read from must be page numbers
+ *   slot, pos            int32 [max_tokens] out (max_tokens may be 0)
+ *   token_start          int32 [num_requests + 1] out: start of every request
+ *                        and the sum of new (values past 2^31 - 1 read 2^31 - 1)
+ *   kv_len               int32 [num_requests] out
+ *   free_head_out        int32 [1] out; may be free_head
+ * kv_len may be cached_len; otherwise outputs must not overlap inputs or each
+ * other.  page_size as in sq_kv_cache, 1 <= max_pages, max_pages * page_size <
+ * 2^31, num_requests * max_pages < 2^31. */
+sq_status sq_kv_plan(const int32_t* cached_len, const int32_t* new_len, int32_t num_requests, int32_t page_size,
+                     const int32_t* free_pages, int32_t num_free, const int32_t* free_head, int32_t* table,
+                     int32_t max_pages, int32_t max_tokens, int32_t* slot, int32_t* pos, int32_t* token_start,
+                     int32_t* kv_len, int32_t* free_head_out, hipStream_t stream);
+
+/* Norm and rotation of queries and keys. */
+typedef struct sq_rope_params {
+  const float* q_weight; /* [head_dim] weight of the queries' norm, or NULL: no norm */
+  const float* k_weight; /* [head_dim] weight of the keys' norm, or NULL: no norm */
+  const float* cos;      /* [num_pos][rot_dim / 2]; NULL when rot_dim is 0 */
+  const float* sin;      /* [num_pos][rot_dim / 2]; NULL when rot_dim is 0 */
+  float eps;             /* >= 0, finite */
+  int32_t num_pos;       /* rows of cos and sin */
+  int32_t rot_dim;       /* leading values of a head that are rotated: a multiple of 16, 0 .. head_dim */
+  int32_t interleaved;   /* pairs (2i, 2i + 1) when not 0, else (i, i + rot_dim / 2) */
+} sq_rope_params;
+
+/* Per token t and head, in fp32 with one rounding at the end:
+ *     u = x * rsqrt(mean(x^2) + eps) * weight      (u = x without a weight)
+ *     (a, b) -> (a cos - b sin, b cos + a sin)     for the pairs of the first rot_dim values,
+ * cos and sin from row pos[t].  Queries go to q_out, keys to k_out and / or
+ * the cache, values to the cache as they are.
+ *   q [T][q_heads][head_dim], k and v [T][kv_heads][head_dim] of dtype, a
+ *     token's heads contiguous, tokens q_stride / k_stride / v_stride elements
+ *     apart (multiples of 8, no less than a token's heads): views of one fused
+ *     qkv output qualify
+ *   pos    int32 [T]; may be NULL when rot_dim is 0.  A token with rot_dim > 0
+ *     whose pos is outside [0, num_pos) is skipped: nothing of it is written
+ *   slot   int32 [T]; a token whose slot is outside the cache leaves it alone.
+ *     Slots in the cache must be distinct.
+ *   q_out  [T][q_heads][head_dim], k_out [T][kv_heads][head_dim] or NULL
+ *   kv     the cache (of this head count, head_dim and dtype), or NULL: then v
+ *     and slot may be NULL and k_out is required
+ * dtype is SQ_OUT_BF16 or SQ_OUT_F16; 0 <= T <= 2^24; q_heads 1 .. 1024;
+ * kv_heads and head_dim as in sq_kv_cache.  Tensors 16-byte aligned, weights,
+ * cos and sin too; outputs must not overlap inputs. */
+sq_status sq_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int32_t T, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                          int32_t dtype, const sq_rope_params* params, const int32_t* pos, const int32_t* slot,
+                          void* q_out, void* k_out, const sq_kv_cache* kv, hipStream_t stream);
+
+/* Bytes of device workspace for sq_attn_paged (partial results of histories
+ * split over workgroups; no initialization needed), at least 256; 0 for
+ * invalid arguments.  Host-only. */
+size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv, int32_t max_kv_len);
+
+/* Attention of one query token per request over the paged cache: with n =
+ * kv_len[r] (clamped to [0, max_kv_len]) and first = max(0, n - window) (0
+ * without a window), query head h reads key-value head h / (q_heads /
+ * num_heads):
+ *     s_j = scale * q . k_j,  out = sum_j exp(s_j) v_j / sum_j exp(s_j),  first <= j < n
+ * and lse = log sum_j exp(s_j).  Token j is row j % page_size of page
+ * table[r][j / page_size]; tokens of a page number outside [0, num_pages) are
+ * not attended.  Where nothing is attended out is 0 and lse -infinity.  Cache
+ * rows that are not attended may hold anything, NaN included.  Sums, maxima
+ * and probabilities' products are carried in fp32 accuracy (probabilities
+ * enter the matrix cores as sums of 16-bit parts); results do not depend on
+ * the run.
+ *   q      [num_requests][q_heads][head_dim] of kv->dtype, requests q_stride
+ *          elements apart (a multiple of 8, no less than a request's heads)
+ *   table  int32 [num_requests][max_pages]
+ *   out    [num_requests][q_heads][head_dim] of out_dtype; lse fp32
+ *          [num_requests][q_heads] or NULL
+ * 0 <= num_requests <= 65536; q_heads a multiple of num_heads, at most 1024;
+ * 0 <= max_kv_len <= max_pages * page_size < 2^31; window >= 0 (0: none);
+ * scale finite.  max_kv_len bounds the work that is launched: the longest
+ * history, or its capacity in a captured graph.  q, out and workspace 16-byte
+ * aligned. */
+sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv,
+                        const int32_t* table, int32_t max_pages, const int32_t* kv_len, int32_t max_kv_len,
+                        int32_t window, float scale, void* out, int32_t out_dtype, float* lse, void* workspace,
+                        size_t ws_bytes, hipStream_t stream);
+
+/* The linear without quantized activations, for few tokens:
+ *     Y = (X D^-1) Q(D W) + b
+ * x bf16 [M][K], dinv fp32 [K] or NULL (16-byte aligned), w the packed int4
+ * weight of the quantized linears, y [M][N] of out_dtype.  x * dinv is rounded
+ * to fp32; it meets the matrix cores as bf16 parts whose sum holds 16
+ * significant bits of it for 16-bit outputs and all 24 for fp32 (x itself
+ * where dinv is NULL), products are exact and sums fp32.  Requires M <= 64
+ * (else SQ_ERR_UNSUPPORTED).  No workspace. */
+sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const sq_weight* w, void* y,
+                          int32_t out_dtype, hipStream_t stream);
+
 /* Measurement hook: the int8 matrix-core rate the GPU sustains, as a
  * ceiling beside the published peak.  Launches sq_probe_mfma_i8_sink_bytes()
  * / 1024 workgroups (two per CU) whose waves each issue back-to-back int8

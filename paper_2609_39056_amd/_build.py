@@ -38,7 +38,8 @@ FLAGS = [
 ]
 
 SOURCES = ["sq_api.cpp", "quant_act.hip", "pack_weights.hip", "gemm_w4.hip", "gemm_skinny.hip", "unfused.hip",
-           "mfma_probe.hip", "calib.hip", "noalloc.hip", "gelu.hip"]
+           "mfma_probe.hip", "calib.hip", "noalloc.hip", "gelu.hip", "kv_plan.hip", "qk_norm_rope.hip",
+           "attn_paged.hip", "linear_w4a16.hip"]
 
 
 _REMARK = re.compile(r"remark: Function Name: (\S+)|remark:\s+(ScratchSize \[bytes/lane\]|VGPRs Spill): (\d+)")

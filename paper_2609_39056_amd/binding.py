@@ -88,8 +88,34 @@ class sq_calib_search_params(ctypes.Structure):
     ]
 
 
+class sq_kv_cache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class sq_rope_params(ctypes.Structure):
+    _fields_ = [
+        ("q_weight", ctypes.c_void_p),
+        ("k_weight", ctypes.c_void_p),
+        ("cos", ctypes.c_void_p),
+        ("sin", ctypes.c_void_p),
+        ("eps", ctypes.c_float),
+        ("num_pos", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+    ]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
 _S = ctypes.c_size_t
 _SIGS = {
     "sq_status_string": (ctypes.c_char_p, [_I]),
@@ -125,6 +151,13 @@ _SIGS = {
     "sq_calib_search_workspace_bytes": (_S, [_I, _I, _I, _I, _I]),
     "sq_calib_search": (_I, [_P, _I, _P, _I, _P, _I, ctypes.POINTER(sq_weight), _P, _P,
                              ctypes.POINTER(sq_calib_search_params), _P, _P, _P, _P, _S, _P]),
+    "sq_kv_plan": (_I, [_P, _P, _I, _I, _P, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P]),
+    "sq_qk_norm_rope": (_I, [_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _I, ctypes.POINTER(sq_rope_params), _P, _P, _P,
+                             _P, ctypes.POINTER(sq_kv_cache), _P]),
+    "sq_attn_workspace_bytes": (_S, [_I, _I, ctypes.POINTER(sq_kv_cache), _I]),
+    "sq_attn_paged": (_I, [_P, _L, _I, _I, ctypes.POINTER(sq_kv_cache), _P, _I, _P, _I, _I, ctypes.c_float, _P, _I, _P,
+                           _P, _S, _P]),
+    "sq_linear_w4a16": (_I, [_P, _I, _P, ctypes.POINTER(sq_weight), _P, _I, _P]),
     "sq_probe_mfma_i8_sink_bytes": (_S, []),
     "sq_probe_mfma_i8": (_I, [_I, _I, _I, _I, _P, _S, _P]),
     "sq_probe_mfma_f8f6": (_I, [_I, _I, _I, _I, _P, _S, _P]),
@@ -490,7 +523,156 @@ def sq_calib_search(x: torch.Tensor, tok2stream: torch.Tensor, num_streams: int,
                                  _ptr(objective_out), wp, wb, _stream(stream)), "sq_calib_search")
 
 
+# ------------------------------------------------------------------ a decoder's token step
+HALF_DTYPES = {torch.bfloat16: SQ_OUT_BF16, torch.float16: SQ_OUT_F16}
+
+
+@dataclass
+class KVCache:
+    """A paged key-value cache on the device."""
+
+    k: torch.Tensor  # bf16 or f16 [num_pages, num_heads, page_size, head_dim]
+    v: torch.Tensor  # the same
+
+    def struct(self) -> sq_kv_cache:
+        if self.k.shape != self.v.shape or self.k.dtype != self.v.dtype or self.k.dtype not in HALF_DTYPES:
+            raise ValueError("keys and values of a cache share one shape and one 16-bit type")
+        pages, heads, page, dim = self.k.shape
+        return sq_kv_cache(_ptr(self.k), _ptr(self.v), pages, heads, page, dim, HALF_DTYPES[self.k.dtype])
+
+
+@dataclass
+class RopeParams:
+    """Norm weights and rotation tables of sq_qk_norm_rope (None: none)."""
+
+    q_weight: Optional[torch.Tensor] = None  # fp32 [head_dim]
+    k_weight: Optional[torch.Tensor] = None  # fp32 [head_dim]
+    eps: float = 1e-6
+    cos: Optional[torch.Tensor] = None       # fp32 [num_pos, rot_dim / 2]
+    sin: Optional[torch.Tensor] = None       # fp32 [num_pos, rot_dim / 2]
+    interleaved: bool = False
+
+    def struct(self, head_dim: int) -> sq_rope_params:
+        _typed(torch.float32, self.q_weight, self.k_weight, self.cos, self.sin)
+        for w in (self.q_weight, self.k_weight):
+            if w is not None and w.shape != (head_dim,):
+                raise ValueError("a norm weight has head_dim values")
+        num_pos = rot = 0
+        if self.cos is not None or self.sin is not None:
+            if self.cos is None or self.sin is None or self.cos.shape != self.sin.shape or self.cos.dim() != 2:
+                raise ValueError("cos and sin are two tables of one shape [num_pos, rot_dim / 2]")
+            num_pos, rot = self.cos.shape[0], 2 * self.cos.shape[1]
+        return sq_rope_params(_ptr(self.q_weight), _ptr(self.k_weight), _ptr(self.cos), _ptr(self.sin), self.eps,
+                              num_pos, rot, int(self.interleaved))
+
+
+def _typed(dtype, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"libsq takes {dtype} here, not {t.dtype}")
+
+
+def _heads(t: torch.Tensor, dtype, T: int, D: int):
+    """Pointer and token stride of [T, heads, D], a token's heads contiguous."""
+    if not t.is_cuda:
+        raise ValueError("libsq takes device tensors")
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype:
+        raise ValueError(f"expected a {dtype} tensor [{T}, heads, {D}]")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != D):
+        raise ValueError("libsq takes tokens whose heads are contiguous")
+    return t.data_ptr(), t.stride(0) if T > 1 else t.shape[1] * D
+
+
+def sq_kv_plan(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: int, free_pages: torch.Tensor,
+               free_head: Optional[torch.Tensor], table: torch.Tensor, slot: torch.Tensor, pos: torch.Tensor,
+               token_start: torch.Tensor, kv_len: torch.Tensor, free_head_out: torch.Tensor, stream=None) -> None:
+    """Block table entries, slots and positions of the requests' new tokens
+    (include/sq.h); every tensor int32, table [R, max_pages], slot and pos
+    [max_tokens]."""
+    _typed(torch.int32, cached_len, new_len, free_pages, free_head, table, slot, pos, token_start, kv_len,
+           free_head_out)
+    R, max_pages = table.shape
+    if (cached_len.shape != (R,) or new_len.shape != (R,) or kv_len.shape != (R,) or token_start.shape != (R + 1,)
+            or slot.dim() != 1 or pos.shape != slot.shape or free_pages.dim() != 1 or free_head_out.numel() < 1
+            or (free_head is not None and free_head.numel() < 1)):
+        raise ValueError("sq_kv_plan: the tensors' sizes do not fit together")
+    _check(lib().sq_kv_plan(_ptr(cached_len), _ptr(new_len), R, page_size, _ptr(free_pages), free_pages.numel(),
+                            _ptr(free_head), _ptr(table), max_pages, slot.numel(), _ptr(slot), _ptr(pos),
+                            _ptr(token_start), _ptr(kv_len), _ptr(free_head_out), _stream(stream)), "sq_kv_plan")
+
+
+def sq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], rope: RopeParams,
+                    pos: Optional[torch.Tensor], slot: Optional[torch.Tensor], q_out: torch.Tensor,
+                    k_out: Optional[torch.Tensor], kv: Optional[KVCache], stream=None) -> None:
+    """Norm and rotation of queries [T, q_heads, D] and keys [T, kv_heads, D]
+    into q_out, k_out and / or the cache, values into the cache
+    (include/sq.h).  q, k and v may be views of one qkv output."""
+    T, Hq, D = q.shape
+    Hk = k.shape[1]
+    qp, qs = _heads(q, q.dtype, T, D)
+    kp, ks = _heads(k, q.dtype, T, D)
+    vp, vs = (None, 0) if v is None else _heads(v, q.dtype, T, D)
+    _typed(torch.int32, pos, slot)
+    for t in (pos, slot):
+        if t is not None and t.shape != (T,):
+            raise ValueError("pos and slot hold one value per token")
+    if (q.dtype not in HALF_DTYPES or q_out.dtype != q.dtype or q_out.shape != (T, Hq, D)
+            or (v is not None and v.shape[1] != Hk)
+            or (k_out is not None and (k_out.dtype != q.dtype or k_out.shape != (T, Hk, D)))):
+        raise ValueError("queries, keys, values and their outputs share one 16-bit type and their sizes")
+    p = rope.struct(D)
+    c = None if kv is None else ctypes.byref(kv.struct())
+    _check(lib().sq_qk_norm_rope(qp, qs, kp, ks, vp, vs, T, Hq, Hk, D, HALF_DTYPES[q.dtype], ctypes.byref(p),
+                                 _ptr(pos), _ptr(slot), _ptr(q_out), _ptr(k_out), c, _stream(stream)),
+           "sq_qk_norm_rope")
+
+
+def sq_attn_workspace_bytes(num_requests: int, q_heads: int, kv: KVCache, max_kv_len: int) -> int:
+    return int(lib().sq_attn_workspace_bytes(num_requests, q_heads, ctypes.byref(kv.struct()), max_kv_len))
+
+
+def sq_attn_paged(q: torch.Tensor, kv: KVCache, table: torch.Tensor, kv_len: torch.Tensor, max_kv_len: int,
+                  window: int, scale: float, out: torch.Tensor, out_dtype: int, lse: Optional[torch.Tensor],
+                  workspace: torch.Tensor, stream=None) -> None:
+    """Attention of one query [R, q_heads, D] per request over the cache's
+    pages table [R, max_pages] (include/sq.h); window 0: none."""
+    c = kv.struct()
+    R, Hq, D = q.shape
+    qp, qs = _heads(q, kv.k.dtype, R, c.head_dim)
+    _typed(torch.int32, table, kv_len)
+    _typed(torch.float32, lse)
+    if (out.shape != q.shape or out.dtype != OUT_DTYPES.get(out_dtype) or table.dim() != 2 or table.shape[0] != R
+            or kv_len.shape != (R,) or (lse is not None and lse.shape != (R, Hq))):
+        raise ValueError("sq_attn_paged: the tensors' sizes or types do not fit together")
+    wp, wb = _ws(workspace)
+    _check(lib().sq_attn_paged(qp, qs, R, Hq, ctypes.byref(c), _ptr(table), table.shape[1], _ptr(kv_len), max_kv_len,
+                               window, scale, _ptr(out), out_dtype, _ptr(lse), wp, wb, _stream(stream)),
+           "sq_attn_paged")
+
+
+def sq_linear_w4a16(x: torch.Tensor, dinv: Optional[torch.Tensor], w: Weight, y: torch.Tensor, out_dtype: int,
+                    stream=None) -> None:
+    """y [M, N] = (x D^-1) Q(D W) + b for at most 64 rows of bf16 x [M, K]
+    (include/sq.h)."""
+    M = x.shape[0]
+    _typed(torch.bfloat16, x)
+    _typed(torch.float32, dinv)
+    if (x.shape != (M, w.K) or y.shape != (M, w.N) or y.dtype != OUT_DTYPES.get(out_dtype)
+            or (dinv is not None and dinv.shape != (w.K,))):
+        raise ValueError("sq_linear_w4a16: the tensors' sizes or types do not fit together")
+    ws = w.struct()
+    _check(lib().sq_linear_w4a16(_ptr(x), M, _ptr(dinv), ctypes.byref(ws), _ptr(y), out_dtype, _stream(stream)),
+           "sq_linear_w4a16")
+
+
 # ------------------------------------------------------------------ helpers
+def alloc_attn_workspace(num_requests: int, q_heads: int, kv: KVCache, max_kv_len: int) -> torch.Tensor:
+    n = sq_attn_workspace_bytes(num_requests, q_heads, kv, max_kv_len)
+    if n == 0:
+        raise ValueError("invalid sizes for an attention workspace")
+    return torch.empty(n, dtype=torch.uint8, device=kv.k.device)
+
+
 def alloc_workspace(variant: int, M: int, K: int, N: int, act_bits: int, device="cuda") -> torch.Tensor:
     n = sq_workspace_bytes(variant, M, K, N, act_bits)
     if n == 0:

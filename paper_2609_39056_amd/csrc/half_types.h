@@ -1,0 +1,57 @@
+// The 16-bit types of the token step's tensors, bf16 and f16: widening is
+// exact, narrowing rounds to nearest even with the hardware conversion (NaN
+// stays NaN).
+#pragma once
+
+#include "sq_internal.h"
+
+namespace sq {
+namespace {
+
+template <bool F16>
+__device__ __forceinline__ float half_lo(uint32_t w) {
+  if constexpr (F16) return f16_to_f32(w & 0xFFFFu);
+  return __uint_as_float(w << 16);
+}
+template <bool F16>
+__device__ __forceinline__ float half_hi(uint32_t w) {
+  if constexpr (F16) return f16_to_f32(w >> 16);
+  return __uint_as_float(w & 0xFFFF0000u);
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t to_half(float v) {
+  if constexpr (F16) return f32_to_f16(v);
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t to_half2(float lo, float hi) {
+  return to_half<F16>(lo) | (to_half<F16>(hi) << 16);
+}
+
+// 8 values of 16 bits <-> 8 floats
+template <bool F16>
+__device__ __forceinline__ void widen8(const uint4& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = half_lo<F16>(w[i]);
+    v[2 * i + 1] = half_hi<F16>(w[i]);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ uint4 narrow8(const float (&v)[8]) {
+  return make_uint4(to_half2<F16>(v[0], v[1]), to_half2<F16>(v[2], v[3]), to_half2<F16>(v[4], v[5]),
+                    to_half2<F16>(v[6], v[7]));
+}
+
+// One output value of SQ_OUT_F32 / BF16 / F16.
+__device__ __forceinline__ void store_out(void* y, size_t i, float v, int32_t out_dtype) {
+  if (out_dtype == SQ_OUT_F32) {
+    static_cast<float*>(y)[i] = v;
+  } else {
+    static_cast<uint16_t*>(y)[i] = static_cast<uint16_t>(out_dtype == SQ_OUT_BF16 ? to_half<false>(v) : to_half<true>(v));
+  }
+}
+
+}  // namespace
+}  // namespace sq

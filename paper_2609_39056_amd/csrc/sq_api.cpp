@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "sq_internal.h"
+#include "token_internal.h"
 
 using namespace sq;
 
@@ -341,6 +342,39 @@ sq_status calib_eval_range(const CalibEval& e, const float* gamma, const float* 
 
 sq_status calib_eval(const CalibEval& e, const float* gamma, const float* clip, double* out, hipStream_t stream) {
   return calib_eval_range(e, gamma, clip, SQ_RANGE_STATIC, out, stream);
+}
+
+}  // namespace
+
+namespace {
+
+// ---------------------------------------------------------------- token step
+bool power_of_two(int32_t v) { return v >= 1 && (v & (v - 1)) == 0; }
+bool valid_page(int32_t P) { return power_of_two(P) && P >= 8 && P <= 1024; }
+int32_t log2_of(int32_t v) { return 31 - __builtin_clz(static_cast<unsigned>(v)); }
+bool valid_dim(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
+bool valid_half(int32_t d) { return d == SQ_OUT_BF16 || d == SQ_OUT_F16; }
+constexpr int64_t kIndexEnd = int64_t{1} << 31;
+constexpr int32_t kMaxRequests = 1 << 16;
+constexpr int32_t kMaxQHeads = 1024, kMaxKvHeads = 256;
+
+sq_status check_cache(const sq_kv_cache* kv) {
+  if (kv == nullptr || kv->k == nullptr || kv->v == nullptr) return SQ_ERR_NULL;
+  if (!valid_half(kv->dtype) || !valid_page(kv->page_size) || !valid_dim(kv->head_dim)) return SQ_ERR_UNSUPPORTED;
+  if (kv->num_heads < 1 || kv->num_heads > kMaxKvHeads || kv->num_pages < 1 ||
+      static_cast<int64_t>(kv->num_pages) * kv->page_size >= kIndexEnd)
+    return SQ_ERR_SHAPE;
+  if (!aligned(kv->k, 16) || !aligned(kv->v, 16)) return SQ_ERR_ALIGN;
+  return SQ_OK;
+}
+
+// Rows of `heads` contiguous heads, `stride` elements apart, in 16-byte pieces.
+bool valid_stride(int64_t stride, int32_t heads, int32_t dim) {
+  return stride >= static_cast<int64_t>(heads) * dim && stride % 8 == 0 && stride <= (int64_t{1} << 40);
+}
+
+bool valid_attn_sizes(int32_t R, int32_t Hq, const sq_kv_cache* kv, int32_t max_kv_len) {
+  return R >= 0 && R <= kMaxRequests && Hq >= 1 && Hq <= kMaxQHeads && Hq % kv->num_heads == 0 && max_kv_len >= 0;
 }
 
 }  // namespace
@@ -816,6 +850,158 @@ sq_status sq_debug_block_acc_i32(const void* qx, int32_t M, int32_t act_bits, co
   if (!aligned(qx, 16) || !aligned(acc_out, 4)) return SQ_ERR_ALIGN;
   GemmArgs g = gemm_args(qx, nullptr, M, nullptr, w, acc_out, SQ_OUT_F32);
   return hip_status(launch_gemm(act_bits, kEpiDump, g, stream));
+}
+
+// ---------------------------------------------------------------- token step
+sq_status sq_kv_plan(const int32_t* cached_len, const int32_t* new_len, int32_t num_requests, int32_t page_size,
+                     const int32_t* free_pages, int32_t num_free, const int32_t* free_head, int32_t* table,
+                     int32_t max_pages, int32_t max_tokens, int32_t* slot, int32_t* pos, int32_t* token_start,
+                     int32_t* kv_len, int32_t* free_head_out, hipStream_t stream) {
+  if (cached_len == nullptr || new_len == nullptr || table == nullptr || token_start == nullptr || kv_len == nullptr ||
+      free_head_out == nullptr)
+    return SQ_ERR_NULL;
+  if ((num_free > 0 && free_pages == nullptr) || (max_tokens > 0 && (slot == nullptr || pos == nullptr)))
+    return SQ_ERR_NULL;
+  if (!valid_page(page_size)) return SQ_ERR_UNSUPPORTED;
+  if (num_requests < 1 || num_requests > kPlanMaxRequests || num_free < 0 || max_tokens < 0 || max_pages < 1 ||
+      static_cast<int64_t>(max_pages) * page_size >= kIndexEnd ||
+      static_cast<int64_t>(num_requests) * max_pages >= kIndexEnd)
+    return SQ_ERR_SHAPE;
+  for (const void* p : {static_cast<const void*>(cached_len), static_cast<const void*>(new_len),
+                        static_cast<const void*>(free_pages), static_cast<const void*>(free_head),
+                        static_cast<const void*>(table), static_cast<const void*>(slot), static_cast<const void*>(pos),
+                        static_cast<const void*>(token_start), static_cast<const void*>(kv_len),
+                        static_cast<const void*>(free_head_out)})
+    if (!aligned(p, 4)) return SQ_ERR_ALIGN;
+  // every workgroup reads the lengths and the head
+  if (kv_len == cached_len || kv_len == new_len || free_head_out == free_head) return SQ_ERR_UNSUPPORTED;
+  PlanArgs a{cached_len, new_len, free_pages, free_head, table, slot, pos, token_start, kv_len, free_head_out,
+             num_requests, max_pages, max_tokens, num_free, log2_of(page_size)};
+  return hip_status(launch_kv_plan(a, stream));
+}
+
+sq_status sq_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int32_t T, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                          int32_t dtype, const sq_rope_params* params, const int32_t* pos, const int32_t* slot,
+                          void* q_out, void* k_out, const sq_kv_cache* kv, hipStream_t stream) {
+  if (params == nullptr) return SQ_ERR_NULL;
+  const sq_rope_params& p = *params;
+  if (!valid_half(dtype) || !valid_dim(head_dim)) return SQ_ERR_UNSUPPORTED;
+  if (T < 0 || T > kMaxM || q_heads < 1 || q_heads > kMaxQHeads || kv_heads < 1 || kv_heads > kMaxKvHeads)
+    return SQ_ERR_SHAPE;
+  if (p.rot_dim < 0 || p.rot_dim > head_dim || p.rot_dim % 16 != 0 || (p.rot_dim > 0 && p.num_pos < 1))
+    return SQ_ERR_SHAPE;
+  if (!std::isfinite(p.eps) || p.eps < 0.0f) return SQ_ERR_UNSUPPORTED;
+  if (kv != nullptr) {
+    const sq_status st = check_cache(kv);
+    if (st != SQ_OK) return st;
+    if (kv->dtype != dtype) return SQ_ERR_UNSUPPORTED;
+    if (kv->num_heads != kv_heads || kv->head_dim != head_dim) return SQ_ERR_SHAPE;
+  }
+  if (T == 0) return SQ_OK;
+  if (q == nullptr || k == nullptr || q_out == nullptr) return SQ_ERR_NULL;
+  if (kv != nullptr ? (v == nullptr || slot == nullptr) : k_out == nullptr) return SQ_ERR_NULL;
+  if (p.rot_dim > 0 && (p.cos == nullptr || p.sin == nullptr || pos == nullptr)) return SQ_ERR_NULL;
+  if (!valid_stride(q_stride, q_heads, head_dim) || !valid_stride(k_stride, kv_heads, head_dim) ||
+      (kv != nullptr && !valid_stride(v_stride, kv_heads, head_dim)))
+    return SQ_ERR_SHAPE;
+  for (const void* t : {q, k, kv != nullptr ? v : nullptr, static_cast<const void*>(p.q_weight),
+                        static_cast<const void*>(p.k_weight), static_cast<const void*>(p.cos),
+                        static_cast<const void*>(p.sin), static_cast<const void*>(q_out),
+                        static_cast<const void*>(k_out)})
+    if (!aligned(t, 16)) return SQ_ERR_ALIGN;
+  if (!aligned(pos, 4) || !aligned(slot, 4)) return SQ_ERR_ALIGN;
+  RopeArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_weight = p.q_weight;
+  a.k_weight = p.k_weight;
+  if (p.rot_dim > 0) {
+    a.cos = p.cos;
+    a.sin = p.sin;
+    a.pos = pos;
+  }
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_out = static_cast<uint16_t*>(k_out);
+  if (kv != nullptr) {
+    a.v = static_cast<const uint16_t*>(v);
+    a.v_stride = v_stride;
+    a.slot = slot;
+    a.k_cache = static_cast<uint16_t*>(kv->k);
+    a.v_cache = static_cast<uint16_t*>(kv->v);
+    a.num_pages = kv->num_pages;
+    a.page_shift = log2_of(kv->page_size);
+  }
+  a.T = T;
+  a.Hq = q_heads;
+  a.Hk = kv_heads;
+  a.D = head_dim;
+  a.rot = p.rot_dim;
+  a.num_pos = p.num_pos;
+  a.eps = p.eps;
+  return hip_status(launch_qk_norm_rope(a, dtype == SQ_OUT_F16, p.interleaved != 0, stream));
+}
+
+size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv, int32_t max_kv_len) {
+  if (check_cache(kv) != SQ_OK || !valid_attn_sizes(num_requests, q_heads, kv, max_kv_len)) return 0;
+  return std::max(kAlign, round_up(attn_partial_bytes(num_requests, q_heads, kv->num_heads, kv->head_dim, max_kv_len)));
+}
+
+sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv,
+                        const int32_t* table, int32_t max_pages, const int32_t* kv_len, int32_t max_kv_len,
+                        int32_t window, float scale, void* out, int32_t out_dtype, float* lse, void* workspace,
+                        size_t ws_bytes, hipStream_t stream) {
+  const sq_status st = check_cache(kv);
+  if (st != SQ_OK) return st;
+  if (!valid_out(out_dtype) || !std::isfinite(scale)) return SQ_ERR_UNSUPPORTED;
+  if (!valid_attn_sizes(num_requests, q_heads, kv, max_kv_len) || window < 0 || max_pages < 1 ||
+      static_cast<int64_t>(max_pages) * kv->page_size >= kIndexEnd ||
+      max_kv_len > static_cast<int64_t>(max_pages) * kv->page_size)
+    return SQ_ERR_SHAPE;
+  if (num_requests == 0) return SQ_OK;
+  if (q == nullptr || table == nullptr || kv_len == nullptr || out == nullptr || workspace == nullptr)
+    return SQ_ERR_NULL;
+  if (!valid_stride(q_stride, q_heads, kv->head_dim)) return SQ_ERR_SHAPE;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(table, 4) || !aligned(kv_len, 4) ||
+      !aligned(lse, 4))
+    return SQ_ERR_ALIGN;
+  if (ws_bytes < sq_attn_workspace_bytes(num_requests, q_heads, kv, max_kv_len)) return SQ_ERR_WORKSPACE;
+  AttnArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(kv->k);
+  a.v = static_cast<const uint16_t*>(kv->v);
+  a.q_stride = q_stride;
+  a.table = table;
+  a.kv_len = kv_len;
+  a.out = out;
+  a.lse = lse;
+  a.part = static_cast<float*>(workspace);
+  a.R = num_requests;
+  a.Hq = q_heads;
+  a.Hk = kv->num_heads;
+  a.D = kv->head_dim;
+  a.max_pages = max_pages;
+  a.num_pages = kv->num_pages;
+  a.page_shift = log2_of(kv->page_size);
+  a.max_kv_len = max_kv_len;
+  a.window = window;
+  a.out_dtype = out_dtype;
+  a.scale = scale;
+  return hip_status(launch_attn_paged(a, kv->dtype == SQ_OUT_F16, stream));
+}
+
+sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const sq_weight* w, void* y,
+                          int32_t out_dtype, hipStream_t stream) {
+  if (x == nullptr || y == nullptr) return SQ_ERR_NULL;
+  const sq_status st = check_weight(w);
+  if (st != SQ_OK) return st;
+  if (!valid_m(M)) return SQ_ERR_SHAPE;
+  if (M > kLinear16MaxM || !valid_out(out_dtype)) return SQ_ERR_UNSUPPORTED;
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(dinv, 16)) return SQ_ERR_ALIGN;
+  const LinearArgs a{x, dinv, w->qw, w->w_scale, w->bias, y, M, w->N, w->K, w->w_group, out_dtype};
+  return hip_status(launch_linear_w4a16(a, stream));
 }
 
 }  // extern "C"
