@@ -1,12 +1,18 @@
 // Block tables and slot maps of a paged key-value cache from request lengths
 // (sq_kv_plan): two exclusive sums over the requests (new tokens, new pages),
 // then one table entry per taken page and one slot and position per token.
+//
+// One launch: every workgroup forms both sums of all requests in its LDS (at
+// most 8192 lengths, from L2) and takes its share of the pages and tokens,
+// found by bisection in the sums, so that one long prompt is spread like many
+// short ones and no workgroup waits for another.  Workgroup 0 writes the
+// per-request outputs.
+#include <algorithm>
+
 #include "token_internal.h"
 
 namespace sq {
 namespace {
-
-constexpr int kPlanThreads = 1024;
 
 __device__ __forceinline__ int32_t saturate(uint64_t v) { return static_cast<int32_t>(v < 0x7FFFFFFFu ? v : 0x7FFFFFFFu); }
 
@@ -50,9 +56,11 @@ __device__ __forceinline__ int owner(const int32_t* sum, int R, int32_t i) {
   return lo;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
-  __shared__ int32_t start[kPlanMaxRequests], first[kPlanMaxRequests];
-  __shared__ uint64_t wave_sum[2][kPlanThreads / 64];
+// THREADS threads for at most MOST requests.
+template <int THREADS, int MOST>
+__global__ __launch_bounds__(THREADS) void kv_plan_kernel(PlanArgs a) {
+  __shared__ int32_t start[MOST], first[MOST];
+  __shared__ uint64_t wave_sum[2][THREADS / 64];
   __shared__ int32_t used;
   const int tid = threadIdx.x, R = a.R;
   const int lane = tid & 63, wave = tid >> 6;
@@ -60,7 +68,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
   if (tid == 0) used = 0;
 
   // a thread sums consecutive requests, the threads' sums are scanned
-  const int per = (R + kPlanThreads - 1) / kPlanThreads;
+  const int per = (R + THREADS - 1) / THREADS;
   const int r0 = min(tid * per, R), r1 = min(r0 + per, R);
   uint64_t tokens = 0, pages = 0;
   for (int r = r0; r < r1; ++r) {
@@ -82,7 +90,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
   uint64_t t_at = t_incl - tokens, p_at = p_incl - pages, t_all = 0, p_all = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) {
       t_at += wave_sum[0][w];
       p_at += wave_sum[1][w];
@@ -90,29 +98,33 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
     t_all += wave_sum[0][w];
     p_all += wave_sum[1][w];
   }
+  const bool writer = blockIdx.x == 0;
   int32_t most = 0;
   for (int r = r0; r < r1; ++r) {
     const Ask q = ask(a, r);
     start[r] = saturate(t_at);
     first[r] = saturate(p_at);
-    const bool ok = placed(a, q, head, first[r], start[r]);
-    if (ok && q.take > 0) most = max(most, first[r] + static_cast<int32_t>(q.take));
-    a.token_start[r] = start[r];
-    a.kv_len[r] = ok ? q.cached + q.fresh : q.cached;
+    if (writer) {
+      const bool ok = placed(a, q, head, first[r], start[r]);
+      if (ok && q.take > 0) most = max(most, first[r] + static_cast<int32_t>(q.take));
+      a.token_start[r] = start[r];
+      a.kv_len[r] = ok ? q.cached + q.fresh : q.cached;
+    }
     t_at += static_cast<uint32_t>(q.fresh);
     p_at += q.take;
   }
-  atomicMax(&used, most);
+  if (most > 0) atomicMax(&used, most);
   __syncthreads();
-  if (tid == 0) {
+  if (writer && tid == 0) {
     a.token_start[R] = saturate(t_all);
     *a.free_head_out = head + used;
   }
 
   // one table entry per page that a placed request takes
   const int32_t pages_end = min(saturate(p_all), a.num_free - head);
-  for (int32_t i = tid; i < pages_end; i += kPlanThreads) {
-    const int r = owner(first, R, i);
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * THREADS + tid, step = static_cast<int64_t>(gridDim.x) * THREADS;
+  for (int64_t i = at; i < pages_end; i += step) {
+    const int r = owner(first, R, static_cast<int32_t>(i));
     const Ask q = ask(a, r);
     if (placed(a, q, head, first[r], start[r]))
       a.table[static_cast<size_t>(r) * a.max_pages + q.have + (i - first[r])] = a.free_pages[head + i];
@@ -120,7 +132,7 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
   // one slot and position per token; fresh pages are read from the free list,
   // not from the table entries written above
   const int32_t tokens_end = saturate(t_all);
-  for (int64_t t = tid; t < a.max_tokens; t += kPlanThreads) {
+  for (int64_t t = at; t < a.max_tokens; t += step) {
     int32_t slot = -1, pos = -1;
     if (t < tokens_end) {
       const int r = owner(start, R, static_cast<int32_t>(t));
@@ -142,7 +154,16 @@ __global__ __launch_bounds__(kPlanThreads) void kv_plan_kernel(PlanArgs a) {
 }  // namespace
 
 hipError_t launch_kv_plan(const PlanArgs& a, hipStream_t s) {
-  kv_plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
+  // one token per thread and pass, at most one workgroup per CU
+  constexpr int32_t kFew = 256;
+  const int threads = a.R <= kFew ? 256 : 1024;
+  const int64_t items = static_cast<int64_t>(a.max_tokens) + a.R;
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((items + threads - 1) / threads, device_cus()));
+  if (a.R <= kFew) {
+    kv_plan_kernel<256, kFew><<<grid, threads, 0, s>>>(a);
+  } else {
+    kv_plan_kernel<1024, kPlanMaxRequests><<<grid, threads, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
