@@ -188,6 +188,7 @@ def _load_call():
                       "(rebuild: python -m paper_2609_39056_amd._build)", RuntimeWarning, stacklevel=3)
         return _NoCall()
     mod.setup(ActParams, Weight)
+    mod.setup_token(KVCache, RopeParams)
     return mod
 
 
@@ -589,6 +590,11 @@ def sq_kv_plan(cached_len: torch.Tensor, new_len: torch.Tensor, page_size: int, 
     """Block table entries, slots and positions of the requests' new tokens
     (include/sq.h); every tensor int32, table [R, max_pages], slot and pos
     [max_tokens]."""
+    L = _lib or lib()
+    st = _call.kv_plan(L.sq_address["sq_kv_plan"], cached_len, new_len, page_size, free_pages, free_head, table, slot,
+                       pos, token_start, kv_len, free_head_out, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_kv_plan")
     _typed(torch.int32, cached_len, new_len, free_pages, free_head, table, slot, pos, token_start, kv_len,
            free_head_out)
     R, max_pages = table.shape
@@ -607,6 +613,10 @@ def sq_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor],
     """Norm and rotation of queries [T, q_heads, D] and keys [T, kv_heads, D]
     into q_out, k_out and / or the cache, values into the cache
     (include/sq.h).  q, k and v may be views of one qkv output."""
+    L = _lib or lib()
+    st = _call.rope(L.sq_address["sq_qk_norm_rope"], q, k, v, rope, pos, slot, q_out, k_out, kv, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_qk_norm_rope")
     T, Hq, D = q.shape
     Hk = k.shape[1]
     qp, qs = _heads(q, q.dtype, T, D)
@@ -636,6 +646,11 @@ def sq_attn_paged(q: torch.Tensor, kv: KVCache, table: torch.Tensor, kv_len: tor
                   workspace: torch.Tensor, stream=None) -> None:
     """Attention of one query [R, q_heads, D] per request over the cache's
     pages table [R, max_pages] (include/sq.h); window 0: none."""
+    L = _lib or lib()
+    st = _call.attn(L.sq_address["sq_attn_paged"], q, kv, table, kv_len, max_kv_len, window, scale, out, out_dtype,
+                    lse, workspace, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_attn_paged")
     c = kv.struct()
     R, Hq, D = q.shape
     qp, qs = _heads(q, kv.k.dtype, R, c.head_dim)
@@ -654,6 +669,10 @@ def sq_linear_w4a16(x: torch.Tensor, dinv: Optional[torch.Tensor], w: Weight, y:
                     stream=None) -> None:
     """y [M, N] = (x D^-1) Q(D W) + b for at most 64 rows of bf16 x [M, K]
     (include/sq.h)."""
+    L = _lib or lib()
+    st = _call.linear16(L.sq_address["sq_linear_w4a16"], x, dinv, w, y, out_dtype, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_linear_w4a16")
     M = x.shape[0]
     _typed(torch.bfloat16, x)
     _typed(torch.float32, dinv)
