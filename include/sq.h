@@ -557,7 +557,7 @@ size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_k
  *   table  int32 [num_requests][max_pages]
  *   out    [num_requests][q_heads][head_dim] of out_dtype; lse fp32
  *          [num_requests][q_heads] or NULL
- * 0 <= num_requests <= 65536; q_heads a multiple of num_heads, at most 1024;
+ * 0 <= num_requests <= 65535; q_heads a multiple of num_heads, at most 1024;
  * 0 <= max_kv_len <= max_pages * page_size < 2^31; window >= 0 (0: none);
  * scale finite.  max_kv_len bounds the work that is launched: the longest
  * history, or its capacity in a captured graph.  q, out and workspace 16-byte

@@ -1,7 +1,6 @@
 // Attention of one new token per request over a paged key-value cache
 // (sq_attn_paged).
-#include <algorithm>
-
+#include "attn_split.h"
 #include "half_types.h"
 #include "token_internal.h"
 
@@ -9,11 +8,11 @@ namespace sq {
 namespace {
 
 constexpr int kWaves = 4;    // of a workgroup
-constexpr int kTile = 32;    // tokens a wave takes at a time
-constexpr int kQTile = 16;   // query heads of a workgroup: the columns of a 16 x 16 matrix-core tile
-constexpr int kMaxChunk = 2048, kMinChunk = 512;
+constexpr int kTile = kAttnTile, kQTile = kAttnQTile;  // kQTile: the columns of a 16 x 16 matrix-core tile
+constexpr int kMinPage = 8;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLowest = -3.402823466e38f;  // no score yet
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -38,26 +37,18 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-// How a history is split over workgroups.
-struct Split {
-  int32_t chunk;  // tokens of a workgroup, a multiple of kTile
-  int32_t count;  // workgroups of a history of `span` tokens
-};
-Split split_of(int64_t heads, int32_t span) {
-  const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads));
-  const int64_t even = (span + want - 1) / want;
-  int64_t chunk = std::min<int64_t>(kMaxChunk, std::max<int64_t>(kMinChunk, (even + 127) / 128 * 128));
-  Split s;
-  s.chunk = static_cast<int32_t>(chunk);
-  s.count = static_cast<int32_t>(std::max<int64_t>(1, (static_cast<int64_t>(span) + chunk - 1) / chunk));
-  return s;
+__device__ __forceinline__ uint4 load16(const uint16_t* p) {
+  typedef unsigned int vec __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const vec*>(p)));
 }
-int64_t max_splits(int64_t heads, int32_t longest) {
-  const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads));
-  return std::max(std::min<int64_t>(want, (static_cast<int64_t>(longest) + kMinChunk - 1) / kMinChunk),
-                  (static_cast<int64_t>(longest) + kMaxChunk - 1) / kMaxChunk);
+// N dwords from a 4-byte boundary.
+template <int N>
+__device__ __forceinline__ void load_words(const uint16_t* p, uint32_t* w) {
+  typedef unsigned int vec __attribute__((ext_vector_type(N), aligned(4)));
+  const vec r = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = r[i];
 }
-int q_tiles(int32_t Hq, int32_t Hk) { return (Hq / Hk + kQTile - 1) / kQTile; }
 
 // The tokens [first, n) of a request.
 __device__ __forceinline__ void range_of(const AttnArgs& a, int r, int& first, int& n) {
@@ -65,46 +56,62 @@ __device__ __forceinline__ void range_of(const AttnArgs& a, int r, int& first, i
   first = a.window > 0 ? max(0, n - a.window) : 0;
 }
 
+// The parts of split histories: values [row][split][D], then maximum and sum
+// [row][split].
+__device__ __forceinline__ float2* part_stats(const AttnArgs& a, const AttnSplit& sp) {
+  return reinterpret_cast<float2*>(a.part + static_cast<size_t>(a.R) * a.Hq * sp.count * a.D);
+}
+
 template <bool F16, int D, int NP>
-__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, Split sp, int qtiles) {
+__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
   constexpr int KF = D / 32;  // fragments of a key row
-  constexpr int E = D / 16;   // dimensions of a lane's part of a value row
+  // a lane's part of a value row: E dimensions, E0 c .. of the first 16 E0 and
+  // E1 c .. of the rest, so that a load covers whole lines across the lanes
+  constexpr int E = D / 16, E0 = E < 8 ? E : 8, E1 = E - E0;
   constexpr int EW = E / 2;   // the same in dwords
+  // The next tile's keys are loaded once this tile's scores are formed, its
+  // values after the products (3 to 4 % at head dimension 128); at 256 the
+  // registers that takes leave one workgroup per CU (58 us, without 50).
+  constexpr bool kAhead = D < 256;
+  constexpr int kPages = kAttnWhole / kMinPage + 1;  // pages of a chunk: one for each of as many threads
+  static_assert(kPages <= 64 * kWaves, "one table entry per thread");
   constexpr float kShift = F16 ? 11.0f : 0.0f;
   constexpr float kSlack = F16 ? 4.0f : 8.0f;
-  __shared__ int32_t pages[kMaxChunk / 8 + 1];
+  __shared__ int32_t pages[kPages];
   __shared__ float s_m[kWaves][kQTile], s_l[kWaves][kQTile], s_o[kWaves][kQTile][D + 4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
 
-  size_t wg = flat_wg();
-  if (wg >= static_cast<size_t>(a.R) * a.Hk * qtiles * sp.count) return;
-  const int kvh = static_cast<int>(wg % a.Hk);
-  wg /= a.Hk;
-  const int qt = static_cast<int>(wg % qtiles);
-  wg /= qtiles;
-  const int split = static_cast<int>(wg % sp.count);
-  const int r = static_cast<int>(wg / sp.count);
+  // blockIdx.x: key-value head, tile of query heads, split; blockIdx.y: request
+  const int r = blockIdx.y;
+  uint32_t wg = blockIdx.x;
+  const int kvh = static_cast<int>(wg % static_cast<uint32_t>(a.Hk));
+  wg /= static_cast<uint32_t>(a.Hk);
+  const int qt = static_cast<int>(wg % static_cast<uint32_t>(qtiles));
+  const int split = static_cast<int>(wg / static_cast<uint32_t>(qtiles));
   const int G = a.Hq / a.Hk;
   const int gq = min(G - qt * kQTile, kQTile);  // query heads here
   const int h0 = kvh * G + qt * kQTile;
 
+  // Without a window the chunk's table entries do not wait for the length
+  // (those past it are in the row all the same, and not used).
   int first, n;
   range_of(a, r, first, n);
-  const int span = n - (first & ~(kTile - 1));
-  const bool whole = span <= sp.chunk;  // one workgroup has all of it
-  if (split > 0 && static_cast<int64_t>(split) * sp.chunk >= span) return;
-  const int begin = (first & ~(kTile - 1)) + split * sp.chunk;
-  const int end = begin + min(n - begin, sp.chunk);
-
+  const int base = a.window > 0 ? first & ~(kTile - 1) : 0;
+  const int64_t begin64 = base + static_cast<int64_t>(split) * sp.chunk;
   const int shift = a.page_shift, mask = (1 << shift) - 1;
+  const int64_t at = (begin64 >> shift) + threadIdx.x;
+  if (threadIdx.x < kPages && at < a.max_pages) {
+    const int32_t p = a.table[static_cast<size_t>(r) * a.max_pages + at];
+    pages[threadIdx.x] = p >= 0 && p < a.num_pages ? p : -1;
+  }
+  const bool whole = n - base <= sp.chunk;  // one workgroup has all of it
+  if (split > 0 && begin64 >= n) return;
+  const int begin = static_cast<int>(begin64);
+  const int end = begin + min(n - begin, sp.chunk);
   const int page0 = begin >> shift;
   const int npages = begin < end ? ((end - 1) >> shift) - page0 + 1 : 0;
-  for (int i = threadIdx.x; i < npages; i += 64 * kWaves) {
-    const int32_t p = a.table[static_cast<size_t>(r) * a.max_pages + page0 + i];
-    pages[i] = p >= 0 && p < a.num_pages ? p : -1;
-  }
 
   // queries: column c is head h0 + c, the lane's values 32 j + 8 g ..
   uint4 q[KF];
@@ -119,37 +126,51 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
   v4f o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = v4f{0, 0, 0, 0};
-  float m = -3.402823466e38f, l = 0.0f;
+  float m = kLowest, l = 0.0f;
   const float scale = a.scale * kLog2e;
 
   auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
   auto row_of = [&](int page, int tok) {
     return ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + (tok & mask);
   };
+  // a tile's keys: tokens b + 16 i + c, the lane's values 32 j + 8 g ..;
+  // its values: tokens b + 16 i + 4 g + x, the lane's dimensions
   const int tiles = (end - begin + kTile - 1) / kTile;
-  for (int t = wave; t < tiles; t += kWaves) {
-    const int b = begin + t * kTile;
-    uint4 k[2][KF];
-    int kp[2];
+  uint4 k[2][KF];
+  uint32_t v[8][EW];
+  int kp[2], vp[2];
+  auto load_k = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int tok = b + 16 * i + c;
       kp[i] = page_of(tok);
       const uint16_t* p = a.k + row_of(kp[i], tok) * D + 8 * g;
 #pragma unroll
-      for (int j = 0; j < KF; ++j) k[i][j] = *reinterpret_cast<const uint4*>(p + 32 * j);
+      for (int j = 0; j < KF; ++j) k[i][j] = load16(p + 32 * j);
     }
-    uint32_t v[8][EW];
-    int vp[2];
+  };
+  auto load_v = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int tok = b + 16 * i + 4 * g;
       vp[i] = page_of(tok);
-      const uint16_t* p = a.v + row_of(vp[i], tok) * D + E * c;
+      const uint16_t* p = a.v + row_of(vp[i], tok) * D;
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int w = 0; w < EW; ++w) v[4 * i + x][w] = reinterpret_cast<const uint32_t*>(p + x * D)[w];
+      for (int x = 0; x < 4; ++x) {
+        load_words<E0 / 2>(p + x * D + E0 * c, v[4 * i + x]);
+        if constexpr (E1 > 0) load_words<E1 / 2>(p + x * D + 16 * E0 + E1 * c, v[4 * i + x] + E0 / 2);
+      }
+    }
+  };
+  if (kAhead && wave < tiles) {
+    load_k(begin + wave * kTile);
+    load_v(begin + wave * kTile);
+  }
+  for (int t = wave; t < tiles; t += kWaves) {
+    const int b = begin + t * kTile;
+    if (!kAhead) {
+      load_k(b);
+      load_v(b);
     }
     v4f s[2];
 #pragma unroll
@@ -161,8 +182,9 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
     float f[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = s[i / 4][i % 4] * scale;
-    const bool full = b >= first && b + kTile <= end && __all(kp[0] >= 0 && kp[1] >= 0);
-    if (!full) {
+    const bool whole_tile = b >= first && b + kTile <= end && __all(kp[0] >= 0 && kp[1] >= 0);
+    if (kAhead && t + kWaves < tiles) load_k(b + kWaves * kTile);
+    if (!whole_tile) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
@@ -207,9 +229,10 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
 #pragma unroll
       for (int u = 0; u < NP; ++u) o[e] = mfma<F16>(vt, make_uint4(p[u][0], p[u][1], p[u][2], p[u][3]), o[e]);
     }
+    if (kAhead && t + kWaves < tiles) load_v(b + kWaves * kTile);
   }
 
-  // the waves' parts: column c, dimensions 4 E g + E x + e
+  // the waves' parts: column c, and the dimensions that lane 4 g + x loaded
   l = quad_sum(l);
   if (g == 0) {
     s_m[wave][c] = m - kShift;
@@ -219,7 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
   for (int e = 0; e < E; ++e)
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-      if (c < gq) s_o[wave][c][E * (4 * g + x) + e] = o[e][x];
+      if (c < gq) s_o[wave][c][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[e][x];
   __syncthreads();
   for (int i = threadIdx.x; i < gq * D; i += 64 * kWaves) {
     const int qh = i / D, d = i % D;
@@ -238,44 +261,129 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
       store_out(a.out, row * D + d, L > 0.0f ? y / L : 0.0f, a.out_dtype);
       if (d == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
     } else {
-      float* part = a.part + (row * sp.count + split) * (D + 2);
-      part[2 + d] = y;
-      if (d == 0) {
-        part[0] = M;
-        part[1] = L;
-      }
+      const size_t part = row * sp.count + split;
+      a.part[part * D + d] = y;
+      if (d == 0) part_stats(a, sp)[part] = make_float2(M, L);
     }
   }
 }
 
-// Joins the parts of one query head of a split history, in their order.
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, Split sp) {
-  const size_t row = flat_wg();
+// Joins the parts of split histories, few of them: a thread takes four
+// dimensions of one query head and its parts in order.
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnSplit sp) {
+  const int D4 = a.D / 4;
+  const size_t i = flat_wg() * 256 + threadIdx.x, row = i / D4;
   if (row >= static_cast<size_t>(a.R) * a.Hq) return;
   int first, n;
   range_of(a, static_cast<int>(row / a.Hq), first, n);
   const int span = n - (first & ~(kTile - 1));
   if (span <= sp.chunk) return;
   const int count = (span + sp.chunk - 1) / sp.chunk;
-  const int D = a.D, d = threadIdx.x;
-  const float* part = a.part + row * sp.count * (D + 2);
-  float M = -3.402823466e38f;
-  for (int s = 0; s < count; ++s) M = fmaxf(M, part[static_cast<size_t>(s) * (D + 2)]);
-  float L = 0.0f, y = 0.0f;
-  for (int s = 0; s < count; ++s) {
-    const float* p = part + static_cast<size_t>(s) * (D + 2);
-    const float al = __builtin_amdgcn_exp2f(p[0] - M);
-    L = __builtin_fmaf(p[1], al, L);
-    if (d < D) y = __builtin_fmaf(p[2 + d], al, y);
+  const int d4 = static_cast<int>(i % D4);
+  const float4* po = reinterpret_cast<const float4*>(a.part) + row * sp.count * D4 + d4;
+  const float2* pm = part_stats(a, sp) + row * sp.count;
+  float M = kLowest, L = 0.0f, v[4] = {0, 0, 0, 0};
+  constexpr int kAhead = 8;  // parts whose loads are in flight together
+  for (int s0 = 0; s0 < count; s0 += kAhead) {
+    float2 ml[kAhead];
+    float4 o[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int s = min(s0 + u, count - 1);
+      ml[u] = pm[s];
+      o[u] = po[static_cast<size_t>(s) * D4];
+      if (s0 + u >= count) ml[u] = make_float2(kLowest, 0.0f);
+    }
+    float mn = M;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) mn = fmaxf(mn, ml[u].x);
+    const float was = __builtin_amdgcn_exp2f(M - mn);
+    M = mn;
+    L *= was;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] *= was;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const float al = s0 + u < count ? __builtin_amdgcn_exp2f(ml[u].x - mn) : 0.0f;
+      L = __builtin_fmaf(ml[u].y, al, L);
+      v[0] = __builtin_fmaf(o[u].x, al, v[0]);
+      v[1] = __builtin_fmaf(o[u].y, al, v[1]);
+      v[2] = __builtin_fmaf(o[u].z, al, v[2]);
+      v[3] = __builtin_fmaf(o[u].w, al, v[3]);
+    }
   }
-  if (d < D) store_out(a.out, row * D + d, L > 0.0f ? y / L : 0.0f, a.out_dtype);
-  if (d == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) store_out(a.out, row * a.D + 4 * d4 + x, L > 0.0f ? v[x] / L : 0.0f, a.out_dtype);
+  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+}
+
+// Joins the parts of a split history, many of them: a workgroup takes 32 dimensions of one
+// query head, eight threads with four dimensions each for every THREADS / 8-th
+// part; their sums are added in a fixed order.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void attn_join_kernel(AttnArgs a, AttnSplit sp) {
+  constexpr int kParts = THREADS / 8, kWavesHere = THREADS / 64;
+  __shared__ float s_max[kWavesHere], s_l[kWavesHere];
+  __shared__ float4 s_sum[kWavesHere][8];
+  const int strips = a.D / 32;
+  const size_t wg = flat_wg(), row = wg / strips;
+  if (row >= static_cast<size_t>(a.R) * a.Hq) return;
+  int first, n;
+  range_of(a, static_cast<int>(row / a.Hq), first, n);
+  const int span = n - (first & ~(kTile - 1));
+  if (span <= sp.chunk) return;
+  const int count = (span + sp.chunk - 1) / sp.chunk;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int d4 = static_cast<int>(wg % strips) * 8 + (tid & 7), D4 = a.D / 4;
+  const float4* po = reinterpret_cast<const float4*>(a.part) + row * sp.count * D4 + d4;
+  const float2* pm = part_stats(a, sp) + row * sp.count;
+  float M = kLowest;
+  for (int s = tid; s < count; s += THREADS) M = fmaxf(M, pm[s].x);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  if (lane == 0) s_max[wave] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWavesHere; ++w) M = fmaxf(M, s_max[w]);
+  float v[5] = {0, 0, 0, 0, 0};
+  for (int s = tid / 8; s < count; s += kParts) {
+    const float2 ml = pm[s];
+    const float4 o = po[static_cast<size_t>(s) * D4];
+    const float al = __builtin_amdgcn_exp2f(ml.x - M);
+    v[0] = __builtin_fmaf(o.x, al, v[0]);
+    v[1] = __builtin_fmaf(o.y, al, v[1]);
+    v[2] = __builtin_fmaf(o.z, al, v[2]);
+    v[3] = __builtin_fmaf(o.w, al, v[3]);
+    v[4] = __builtin_fmaf(ml.y, al, v[4]);
+  }
+#pragma unroll
+  for (int o = 8; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] += __shfl_xor(v[i], o, 64);
+  if (lane < 8) {
+    s_sum[wave][lane] = make_float4(v[0], v[1], v[2], v[3]);
+    if (lane == 0) s_l[wave] = v[4];
+  }
+  __syncthreads();
+  if (tid >= 8) return;
+  for (int w = 1; w < kWavesHere; ++w) {
+    const float4 o = s_sum[w][tid];
+    v[0] += o.x;
+    v[1] += o.y;
+    v[2] += o.z;
+    v[3] += o.w;
+    v[4] += s_l[w];
+  }
+  const float L = v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) store_out(a.out, row * a.D + 4 * d4 + i, L > 0.0f ? v[i] / L : 0.0f, a.out_dtype);
+  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
 template <bool F16, int NP>
-void launch_dim(const AttnArgs& a, const Split& sp, hipStream_t s) {
-  const int qt = q_tiles(a.Hq, a.Hk);
-  const dim3 grid = wg_grid(static_cast<size_t>(a.R) * a.Hk * qt * sp.count);
+void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
+  const int qt = (a.Hq / a.Hk + kQTile - 1) / kQTile;
+  const dim3 grid(static_cast<unsigned>(a.Hk * qt * sp.count), static_cast<unsigned>(a.R));
   switch (a.D) {
     case 64: attn_kernel<F16, 64, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
     case 96: attn_kernel<F16, 96, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
@@ -288,14 +396,14 @@ void launch_dim(const AttnArgs& a, const Split& sp, hipStream_t s) {
 }  // namespace
 
 size_t attn_partial_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t max_kv_len) {
-  const int64_t splits = max_splits(static_cast<int64_t>(R) * Hk * q_tiles(Hq, Hk), max_kv_len);
-  return splits <= 1 ? 0 : static_cast<size_t>(R) * Hq * splits * (D + 2) * 4;
+  return attn_part_bytes(R, Hq, D, attn_most_splits(attn_heads(R, Hq, Hk), max_kv_len));
 }
 
 hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
-  const int32_t span = a.window > 0 ? static_cast<int32_t>(std::min<int64_t>(a.max_kv_len, a.window + int64_t{kTile - 1}))
-                                    : a.max_kv_len;
-  const Split sp = split_of(static_cast<int64_t>(a.R) * a.Hk * q_tiles(a.Hq, a.Hk), span);
+  const int64_t heads = attn_heads(a.R, a.Hq, a.Hk);
+  const AttnSplit sp = attn_split(heads, attn_span(a.max_kv_len, a.window));
+  if (attn_part_bytes(a.R, a.Hq, a.D, sp.count) > a.part_bytes) return hipErrorInvalidValue;
+  if (heads / a.R * sp.count >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
   if (f16)
     launch_dim<true, 2>(a, sp, s);
   else if (a.out_dtype == SQ_OUT_F32)
@@ -304,7 +412,15 @@ hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
     launch_dim<false, 2>(a, sp, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.count == 1) return e;
-  attn_join_kernel<<<wg_grid(static_cast<size_t>(a.R) * a.Hq), 256, 0, s>>>(a, sp);
+  const dim3 rows = wg_grid(static_cast<size_t>(a.R) * a.Hq * (a.D / 32));
+  if (sp.count <= 32) {
+    const size_t n = static_cast<size_t>(a.R) * a.Hq * (a.D / 4);
+    attn_join_few_kernel<<<wg_grid((n + 255) / 256), 256, 0, s>>>(a, sp);
+  } else if (sp.count <= 64) {
+    attn_join_kernel<256><<<rows, 256, 0, s>>>(a, sp);
+  } else {
+    attn_join_kernel<1024><<<rows, 1024, 0, s>>>(a, sp);
+  }
   return hipGetLastError();
 }
 

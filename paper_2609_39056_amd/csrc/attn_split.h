@@ -1,0 +1,66 @@
+// How the paged attention splits histories over workgroups (host C++, no HIP).
+//
+// A workgroup costs about 5 us from its launch to its last store (three
+// dependent loads, the join of its waves) and 1.2 us per 128 tokens; a split
+// adds a second kernel, 3 to 6 us.  So short spans stay whole: up to 384
+// tokens, or up to 1280 where the (request, head) pairs alone fill the CUs (768
+// heads with 1055 tokens: 38 us whole, 42 in five parts, 47 in two; 1024 heads
+// with up to 1000: 55 whole, 68 in two).  Longer ones aim at 2048 workgroups in
+// all, eight per CU, so that ragged batches even out: 512 heads with 1024 to
+// 8192 tokens take 176 us in chunks of 512, 193 in 1024, 212 in 1152.  Spans
+// past 65536 may take chunks of 1024 (two histories of 131072, 8 heads: 136 us,
+// 142 in chunks of 512: half the parts to join).
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace sq {
+
+constexpr int32_t kAttnWhole = 1280;      // the longest span that is ever left whole
+constexpr int32_t kAttnQTile = 16;        // query heads of a workgroup
+constexpr int32_t kAttnTile = 32;         // tokens a wave takes at a time; spans start at a multiple of it
+
+struct AttnSplit {
+  int32_t chunk;  // tokens of a workgroup
+  int32_t count;  // workgroups of a history of the whole span
+};
+
+// Workgroups per split: requests x key-value heads x tiles of query heads.
+inline int64_t attn_heads(int32_t R, int32_t Hq, int32_t Hk) {
+  return static_cast<int64_t>(R) * Hk * ((Hq / Hk + kAttnQTile - 1) / kAttnQTile);
+}
+inline int64_t attn_wanted(int64_t heads) { return std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads)); }
+inline bool attn_whole(int64_t heads, int64_t span) { return span <= (heads >= 192 ? kAttnWhole : 384); }
+constexpr int64_t kAttnLeastShort = 128, kAttnLeast = 256, kAttnMost = 512, kAttnMostLong = 1024;
+constexpr int64_t kAttnShort = 4096, kAttnLong = 65536;
+
+inline AttnSplit attn_split(int64_t heads, int64_t span) {
+  if (attn_whole(heads, span)) return {kAttnWhole, 1};
+  const int64_t want = attn_wanted(heads);
+  const int64_t even = ((span + want - 1) / want + 127) / 128 * 128;
+  const int64_t least = span <= kAttnShort ? kAttnLeastShort : kAttnLeast;
+  const int64_t chunk = std::min(span <= kAttnLong ? kAttnMost : kAttnMostLong, std::max(least, even));
+  return {static_cast<int32_t>(chunk), static_cast<int32_t>((span + chunk - 1) / chunk)};
+}
+
+// No span up to `longest` is split into more parts.
+inline int64_t attn_most_splits(int64_t heads, int64_t longest) {
+  if (attn_whole(heads, longest)) return 1;
+  const int64_t least = std::max((longest + kAttnLeast - 1) / kAttnLeast,
+                                 (std::min(longest, kAttnShort) + kAttnLeastShort - 1) / kAttnLeastShort);
+  return std::max(std::min(attn_wanted(heads), least), (longest + kAttnMost - 1) / kAttnMost);
+}
+
+// Bytes of the parts: head_dim values, a maximum and a sum each.
+inline size_t attn_part_bytes(int32_t R, int32_t Hq, int32_t D, int64_t splits) {
+  return splits <= 1 ? 0 : static_cast<size_t>(R) * Hq * static_cast<size_t>(splits) * (D + 2) * 4;
+}
+
+// Tokens a call may attend per request, from a multiple of kAttnTile on.
+inline int64_t attn_span(int32_t max_kv_len, int32_t window) {
+  return window > 0 ? std::min<int64_t>(max_kv_len, static_cast<int64_t>(window) + kAttnTile - 1) : max_kv_len;
+}
+
+}  // namespace sq

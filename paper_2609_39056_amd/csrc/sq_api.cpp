@@ -355,7 +355,7 @@ int32_t log2_of(int32_t v) { return 31 - __builtin_clz(static_cast<unsigned>(v))
 bool valid_dim(int32_t d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
 bool valid_half(int32_t d) { return d == SQ_OUT_BF16 || d == SQ_OUT_F16; }
 constexpr int64_t kIndexEnd = int64_t{1} << 31;
-constexpr int32_t kMaxRequests = 1 << 16;
+constexpr int32_t kMaxRequests = 65535;  // a grid's y dimension
 constexpr int32_t kMaxQHeads = 1024, kMaxKvHeads = 256;
 
 sq_status check_cache(const sq_kv_cache* kv) {
@@ -978,6 +978,7 @@ sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, i
   a.out = out;
   a.lse = lse;
   a.part = static_cast<float*>(workspace);
+  a.part_bytes = ws_bytes;
   a.R = num_requests;
   a.Hq = q_heads;
   a.Hk = kv->num_heads;

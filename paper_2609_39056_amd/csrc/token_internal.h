@@ -31,7 +31,8 @@ struct AttnArgs {
   const int32_t *table, *kv_len;
   void* out;
   float* lse;   // or NULL
-  float* part;  // partial results of split histories
+  float* part;  // partial results of split histories, part_bytes of them
+  size_t part_bytes;
   int32_t R, Hq, Hk, D, max_pages, num_pages, page_shift, max_kv_len, window, out_dtype;
   float scale;
 };

@@ -1,0 +1,71 @@
+"""How the paged attention splits histories (csrc/attn_split.h), asked on the
+host: what has to hold for every size."""
+import random
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2609_39056_amd import _build
+
+SRC = """
+#include "attn_split.h"
+#include <stdio.h>
+using namespace sq;
+int main() {
+  int R, Hq, Hk, longest, window;
+  while (scanf("%d %d %d %d %d", &R, &Hq, &Hk, &longest, &window) == 5) {
+    const long long heads = attn_heads(R, Hq, Hk), span = attn_span(longest, window);
+    const AttnSplit s = attn_split(heads, span);
+    printf("%lld %lld %d %d %lld %zu\\n", heads, span, s.chunk, s.count, (long long)attn_most_splits(heads, longest),
+           attn_part_bytes(R, Hq, 128, attn_most_splits(heads, longest)));
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def split(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("clang++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    d = tmp_path_factory.mktemp("split")
+    (d / "split.cpp").write_text(SRC)
+    subprocess.run([cxx, "-std=c++17", "-O1", f"-I{_build.CSRC}", str(d / "split.cpp"), "-o", str(d / "split")], check=True)
+
+    def ask(rows):
+        text = "\n".join(" ".join(map(str, r)) for r in rows) + "\n"
+        out = subprocess.run([str(d / "split")], input=text, capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+
+    return ask
+
+
+def cases():
+    rng = random.Random(5)
+    edges = [0, 1, 31, 32, 33, 383, 384, 385, 1279, 1280, 1281, 4095, 4096, 4097, 65535, 65536, 65537, 131072, 2 ** 31 - 1]
+    for R, Hq, Hk in ((1, 1, 1), (1, 16, 16), (1, 8, 1), (1, 32, 1), (2, 32, 8), (24, 8, 8), (64, 40, 8), (65535, 1024, 256)):
+        for n in edges:
+            for w in (0, 1, 353, 354, 1249, 1250, 2 ** 31 - 1):
+                yield R, Hq, Hk, n, w
+    for _ in range(20000):
+        Hk = rng.randint(1, 40)
+        yield (int(2 ** rng.uniform(0, 14)), Hk * rng.randint(1, 20), Hk, int(2 ** rng.uniform(0, 31)) - 1,
+               rng.choice([0, 0, int(2 ** rng.uniform(0, 30))]))
+
+
+def test_every_split_covers_its_span_and_fits_the_workspace(split):
+    asked = list(cases())
+    for (R, Hq, Hk, longest, window), (heads, span, chunk, count, most, nbytes) in zip(asked, split(asked)):
+        what = (R, Hq, Hk, longest, window)
+        assert heads == R * Hk * -(-(Hq // Hk) // 16), what
+        # any window [n - window, n) from a multiple of 32 on, any n up to the longest
+        assert span == (longest if window == 0 else min(longest, window + 31)), what
+        assert count >= 1 and chunk * count >= span and (count == 1 or chunk * (count - 1) < span), what
+        # a chunk's pages of 8 tokens and one more fit the kernel's table of 161
+        assert chunk <= 1280 and (count == 1 or chunk % 128 == 0), what
+        # the workspace is sized without the window
+        assert count <= most, what
+        assert nbytes == (0 if most == 1 else R * Hq * most * 130 * 4), what
+        if count == 1 and span > 0:
+            assert chunk >= span, what

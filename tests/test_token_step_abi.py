@@ -93,7 +93,7 @@ def attn(L, kv=None, no_cache=False, **kw):  # noqa: F811
 @pytest.mark.parametrize("kw,code", [
     (dict(no_cache=True), NULL), (dict(q=None), NULL), (dict(table=None), NULL), (dict(kv_len=None), NULL),
     (dict(out=None), NULL), (dict(ws=None), NULL), (dict(out_dtype=3), UNSUP), (dict(scale=NAN), UNSUP),
-    (dict(scale=INF), UNSUP), (dict(R=-1), SHAPE), (dict(R=65537), SHAPE), (dict(Hq=0), SHAPE), (dict(Hq=15), SHAPE),
+    (dict(scale=INF), UNSUP), (dict(R=-1), SHAPE), (dict(R=65536), SHAPE), (dict(Hq=0), SHAPE), (dict(Hq=15), SHAPE),
     (dict(Hq=1026), SHAPE), (dict(n=-1), SHAPE), (dict(n=129), SHAPE), (dict(window=-1), SHAPE),
     (dict(max_pages=0), SHAPE), (dict(max_pages=1 << 27), SHAPE), (dict(qs=2040), SHAPE), (dict(qs=2049), SHAPE),
     (dict(q=A + 8), ALIGN), (dict(out=A + 8), ALIGN), (dict(ws=A + 8), ALIGN), (dict(table=A + 2), ALIGN),
@@ -107,7 +107,7 @@ def test_attn_workspace(L):  # noqa: F811
     def n(R, Hq, length, **kw):
         return L.sq_attn_workspace_bytes(R, Hq, ctypes.byref(cache(**kw)), length)
 
-    for args in ((1, 16, 0), (1, 16, 1), (64, 16, 8192), (2, 32, 131072), (65536, 2, 2 ** 31 - 1)):
+    for args in ((1, 16, 0), (1, 16, 1), (64, 16, 8192), (2, 32, 131072), (65535, 2, 2 ** 31 - 1)):
         assert n(*args) >= 256 and n(*args) % 256 == 0
     assert n(1, 15, 100) == 0 and n(-1, 16, 100) == 0 and n(1, 16, -1) == 0 and n(1, 16, 100, page_size=3) == 0
     assert L.sq_attn_workspace_bytes(1, 16, None, 100) == 0
