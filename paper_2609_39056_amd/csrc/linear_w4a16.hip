@@ -14,6 +14,7 @@
 // order through LDS.
 #include <algorithm>
 
+#include "gemm_frag.h"
 #include "half_types.h"
 #include "token_internal.h"
 
@@ -84,56 +85,66 @@ __device__ __forceinline__ void load_block(const LinearArgs& a, int n0, int b, B
   const uint16_t* step = a.w_scale + static_cast<size_t>((b * kBlock) / a.w_group) * a.N + n0 + c;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    o.w[t] = *reinterpret_cast<const uint4*>(a.qw + static_cast<size_t>(n0 + 16 * t + c) * (a.K / 2) + b * (kBlock / 2) + 16 * g);
+    const uint8_t* row = a.qw + static_cast<size_t>(n0 + 16 * t + c) * (a.K / 2);
+    o.w[t] = *reinterpret_cast<const uint4*>(row + b * (kBlock / 2) + 16 * g);
     o.step[t] = step[16 * t];
   }
 }
 
-// total += Delta * (block sums) of the rows whose fragments f[0 .. 4) hold.
-template <int NT, int NP>
-__device__ __forceinline__ void add_block(const uint4 (&f)[4][NP], const Block<NT>& blk, v4f (&total)[NT]) {
+// total += Delta * (block sums); fragment(j) gives the NP parts of the rows at
+// the lane's channels 8 j ..
+template <int NT, int NP, typename Fragment>
+__device__ __forceinline__ void add_block(Fragment fragment, const Block<NT>& blk, v4f (&total)[NT]) {
   const uint4 m8 = make_uint4(kMinus8, kMinus8, kMinus8, kMinus8);
-  v4f base = v4f{0, 0, 0, 0};
+  v4f base = v4f{0, 0, 0, 0}, acc[NT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int t = 0; t < NT; ++t) acc[t] = v4f{0, 0, 0, 0};
 #pragma unroll
-    for (int u = 0; u < NP; ++u) base = mfma(f[j][u], m8, base);
+  for (int j = 0; j < 4; ++j) {
+    uint4 f[NP];
+    fragment(j, f);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    v4f acc = base;
-    const uint32_t w[4] = {blk.w[t].x, blk.w[t].y, blk.w[t].z, blk.w[t].w};
+    for (int u = 0; u < NP; ++u) base = mfma(f[u], m8, base);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int t = 0; t < NT; ++t) {
+      const uint32_t w[4] = {blk.w[t].x, blk.w[t].y, blk.w[t].z, blk.w[t].w};
       const uint4 codes = widen_codes(w[j]);
 #pragma unroll
-      for (int u = 0; u < NP; ++u) acc = mfma(f[j][u], codes, acc);
+      for (int u = 0; u < NP; ++u) acc[t] = mfma(f[u], codes, acc[t]);
     }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
     const float step = f16_to_f32(blk.step[t]) * kCodeUnit;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf(acc[i], step, total[t][i]);
+    for (int i = 0; i < 4; ++i) total[t][i] = __builtin_fmaf(acc[t][i] + base[i], step, total[t][i]);
   }
 }
 
-// Adds the waves' sums (rows m * np .. + np make output row m), bias, store.
+// Adds the waves' sums (tile rows m * np .. + np make output row m0 + m), bias,
+// store.
 template <int NT>
-__device__ __forceinline__ void finish(const LinearArgs& a, const float* sums, int waves, int rows, int np, int n0) {
-  for (int i = threadIdx.x; i < a.M * 16 * NT; i += blockDim.x) {
-    const int m = i / (16 * NT), t = (i / 16) % NT, c = i % 16;
+__device__ __forceinline__ void finish(const LinearArgs& a, const float* sums, int waves, int tile_rows, int np, int m0,
+                                       int rows, int n0) {
+  for (int i = threadIdx.x; i < rows * 16 * NT; i += blockDim.x) {
+    const int m = i / (16 * NT), t = (i / 16) % NT, c = i % 16, n = n0 + 16 * t + c;
+    const float bias = a.bias != nullptr ? bf16_to_f32(a.bias[n]) : 0.0f;
     float y = 0.0f;
-    for (int w = 0; w < waves; ++w)
-      for (int u = 0; u < np; ++u) y += sums[((w * NT + t) * rows + m * np + u) * 16 + c];
-    const int n = n0 + 16 * t + c;
-    if (a.bias != nullptr) y += bf16_to_f32(a.bias[n]);
-    store_out(a.y, static_cast<size_t>(m) * a.N + n, y, a.out_dtype);
+    for (int u = 0; u < np; ++u) {
+      const float* p = sums + (t * tile_rows + m * np + u) * 16 + c;
+#pragma unroll 4
+      for (int w = 0; w < waves; ++w) y += p[w * NT * tile_rows * 16];
+    }
+    store_out(a.y, static_cast<size_t>(m0 + m) * a.N + n, a.bias != nullptr ? y + bias : y, a.out_dtype);
   }
 }
 
-// Few rows (M * NP <= 16): the parts of x~ are rows of one matrix-core tile.
-// The workgroup stages them for `iters` blocks per wave at a time in LDS, in
-// 16-byte pieces ((block * 4 + j) * 4 + g) * R + row, so every x~ is split
-// once per workgroup and a wave reads its fragments as whole lines.
+// Few rows (M * NP <= 16, all of x~ in 64 KB): the parts of x~ are rows of one
+// matrix-core tile.  The workgroup stages them in LDS, in 16-byte pieces
+// ((block * 4 + j) * 4 + g) * R + row, so every x~ is split once per workgroup
+// and only as many rows as there are; the wave's next block is loaded ahead.
 template <int NP, int NT>
-__global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a, int iters) {
+__global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   uint4* stage = reinterpret_cast<uint4*>(lds);
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -145,30 +156,25 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a, int i
   for (int t = 0; t < NT; ++t) total[t] = v4f{0, 0, 0, 0};
   Block<NT> next;
   if (wave < nblk) load_block<NT>(a, n0, wave, next);
-  for (int b0 = 0; b0 < nblk; b0 += iters * waves) {
-    const int blocks = min(iters * waves, nblk - b0);
-    if (b0 > 0) __syncthreads();
-    for (int i = threadIdx.x; i < blocks * 16 * a.M; i += blockDim.x) {
-      const int piece = i % (blocks * 16), m = i / (blocks * 16);
-      const int k = b0 * kBlock + piece * 8;
-      uint4 p[NP];
-      parts_of<NP>(*reinterpret_cast<const uint4*>(a.x + static_cast<size_t>(m) * a.K + k), a.dinv + k, p);
-      const int at = ((piece / 16) * 16 + (piece & 3) * 4 + ((piece >> 2) & 3)) * R + m * NP;
+  const int pieces = nblk * 16;
+  for (int i = threadIdx.x; i < pieces * a.M; i += blockDim.x) {
+    const int piece = i % pieces, m = i / pieces;
+    uint4 p[NP];
+    parts_of<NP>(*reinterpret_cast<const uint4*>(a.x + static_cast<size_t>(m) * a.K + piece * 8), a.dinv + piece * 8, p);
+    const int at = ((piece / 16) * 16 + (piece & 3) * 4 + ((piece >> 2) & 3)) * R + m * NP;
 #pragma unroll
-      for (int u = 0; u < NP; ++u) stage[at + u] = p[u];
-    }
-    __syncthreads();
-    for (int b = wave; b < blocks; b += waves) {
-      const Block<NT> blk = next;
-      if (b0 + b + waves < nblk) load_block<NT>(a, n0, b0 + b + waves, next);
-      uint4 f[4][1];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f[j][0] = make_uint4(0, 0, 0, 0);
-        if (c < R) f[j][0] = stage[(b * 16 + j * 4 + g) * R + c];
-      }
-      add_block<NT, 1>(f, blk, total);
-    }
+    for (int u = 0; u < NP; ++u) stage[at + u] = p[u];
+  }
+  __syncthreads();
+  for (int b = wave; b < nblk; b += waves) {
+    const Block<NT> blk = next;
+    if (b + waves < nblk) load_block<NT>(a, n0, b + waves, next);
+    add_block<NT, 1>(
+        [&](int j, uint4(&f)[1]) {
+          f[0] = make_uint4(0, 0, 0, 0);
+          if (c < R) f[0] = stage[(b * 16 + j * 4 + g) * R + c];
+        },
+        blk, total);
   }
   __syncthreads();
   float* sums = reinterpret_cast<float*>(lds);
@@ -177,40 +183,115 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a, int i
 #pragma unroll
     for (int i = 0; i < 4; ++i) sums[((wave * NT + t) * 16 + 4 * g + i) * 16 + c] = total[t][i];
   __syncthreads();
-  finish<NT>(a, sums, waves, 16, NP, n0);
+  finish<NT>(a, sums, waves, 16, NP, 0, a.M, n0);
 }
 
-// More rows: RT tiles of 16 rows, whose parts each wave splits in registers
-// as it needs them (rows past M repeat the last one and are not stored).
+// More rows: RT tiles of 16 rows.  Each wave copies its blocks (activation
+// rows, weights, weight steps and the channel scaling) by direct global -> LDS
+// loads into a ring of its own, SLOTS - 1 blocks ahead, and splits x~ in
+// registers as it takes the fragments.  The copies go along the rows, four
+// rows of 256 bytes (16 of 64) per instruction; loads in the fragments' own
+// layout touch a line with every lane, and those kept the address unit busy for
+// the whole kernel (16 rows of 13824 -> 5120 channels: 23 us without a
+// channel scaling, 33 with one).  Rows past M repeat the last one and are not
+// stored.  A wave reads only what it copied: the loop has no barriers.
 template <int NP, int NT, int RT>
-__global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+struct Ring {
+  static constexpr int X = RT * 16 * 2 * kBlock;    // row r, 16-byte chunk k at r * 256 + 16 * (k ^ (r & 15))
+  static constexpr int W = NT * 16 * (kBlock / 2);  // channel n, chunk k at n * 64 + 16 * (k ^ ((n >> 2) & 3))
+  static constexpr int X_OFF = 0, W_OFF = X, S_OFF = X + W, D_OFF = S_OFF + 256;
+  static constexpr int SLOT = D_OFF + (NP > 1 ? 4 * kBlock : 0);
+  static constexpr int COPIES = RT * 4 + NT + 1 + (NP > 1 ? 2 : 0);
+  // blocks in the ring and waves of a workgroup.  Twelve waves without a block
+  // ahead hide the latency better than eight with one (16 rows of 13824 -> 5120,
+  // scaled, fp32: 30.2 and 31.1 us; sixteen spill registers, 29.3 to 30.2); the
+  // wider strips of NT = 4 take eight (5120 -> 15360: 17.1, 19 with twelve)
+  static constexpr int SLOTS = RT == 1 && NT <= 2 ? 1 : 2;
+  static constexpr int WAVES = RT == 1 ? (NT <= 2 ? 12 : 8) : 4;
+  static_assert(WAVES * SLOTS * SLOT <= 160 * 1024, "the rings fit in the LDS");
+  static_assert(NT * RT * 1024 <= SLOTS * SLOT, "the waves' sums fit in the rings");
+};
+
+template <int NP, int NT, int RT>
+__global__ __launch_bounds__((64 * Ring<NP, NT, RT>::WAVES)) void linear_rows_kernel(LinearArgs a) {
+  using L = Ring<NP, NT, RT>;
+  __shared__ __attribute__((aligned(16))) uint8_t ring[L::WAVES][L::SLOTS][L::SLOT];
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nblk = a.K / kBlock;
-  const int n0 = blockIdx.x * 16 * NT;
+  const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * RT;
+  const int rows = min(a.M - m0, 16 * RT);
+  const uint16_t* xs = a.x + static_cast<size_t>(m0) * a.K;
+  uint32_t xoff[RT * 4], woff[NT];
+#pragma unroll
+  for (int i = 0; i < RT * 4; ++i) {
+    const int r = 4 * i + g;
+    xoff[i] = static_cast<uint32_t>(min(r, rows - 1) * a.K * 2 + 16 * (c ^ (r & 15)));
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int n = 16 * t + (lane >> 2);
+    woff[t] = static_cast<uint32_t>(n * (a.K / 2) + 16 * ((lane & 3) ^ ((n >> 2) & 3)));
+  }
+  const uint32_t soff = 4 * (lane & (8 * NT - 1));  // lanes past the steps repeat them
+  const uint32_t ring0 = lds_offset(&ring[wave][0][0]);
+  const uint8_t* qw = a.qw + static_cast<size_t>(n0) * (a.K / 2);
+  auto copy = [&](int b, int slot) {
+    const uint32_t at = ring0 + slot * L::SLOT;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) dma<16>(qw + b * (kBlock / 2), woff[t], at + L::W_OFF + t * 1024);
+    dma<4>(a.w_scale + static_cast<size_t>((b * kBlock) / a.w_group) * a.N + n0, soff, at + L::S_OFF);
+#pragma unroll
+    for (int i = 0; i < RT * 4; ++i) dma<16>(xs + b * kBlock, xoff[i], at + L::X_OFF + i * 1024);
+    if constexpr (NP > 1) {
+      dma<4>(a.dinv + b * kBlock, 4 * lane, at + L::D_OFF);
+      dma<4>(a.dinv + b * kBlock + 64, 4 * lane, at + L::D_OFF + 256);
+    }
+  };
   v4f total[RT][NT];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int t = 0; t < NT; ++t) total[r][t] = v4f{0, 0, 0, 0};
-  Block<NT> next;
-  if (wave < nblk) load_block<NT>(a, n0, wave, next);
-  for (int b = wave; b < nblk; b += waves) {
-    const Block<NT> blk = next;
-    if (b + waves < nblk) load_block<NT>(a, n0, b + waves, next);
-    const int k = b * kBlock + 32 * g;
+
+  constexpr int DIST = L::SLOTS - 1;  // blocks ahead
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const uint16_t* x = a.x + static_cast<size_t>(min(16 * r + c, a.M - 1)) * a.K + k;
-      uint4 f[4][NP];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        parts_of<NP>(*reinterpret_cast<const uint4*>(x + 8 * j), a.dinv + k + 8 * j, f[j]);
-      add_block<NT, NP>(f, blk, total[r]);
+  for (int u = 0; u < DIST; ++u)
+    if (wave + u * L::WAVES < nblk) copy(wave + u * L::WAVES, u);
+  int slot = 0;
+  for (int b = wave; b < nblk; b += L::WAVES) {
+    // the slot that is filled next was read in the last pass: its reads are done
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (DIST == 0) {
+      copy(b, 0);
+      wait_vm<0>();
+    } else if (b + DIST * L::WAVES < nblk) {
+      copy(b + DIST * L::WAVES, slot == 0 ? DIST : slot - 1);
+      wait_vm<DIST * L::COPIES>();
+    } else {
+      wait_vm<0>();
     }
+    const uint8_t* st = &ring[wave][slot][0];
+    Block<NT> blk;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int n = 16 * t + c;
+      blk.w[t] = *reinterpret_cast<const uint4*>(st + L::W_OFF + n * 64 + 16 * (g ^ ((n >> 2) & 3)));
+      blk.step[t] = *reinterpret_cast<const uint16_t*>(st + L::S_OFF + 2 * n);
+    }
+    const float* d = reinterpret_cast<const float*>(st + L::D_OFF) + 32 * g;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+      add_block<NT, NP>(
+          [&](int j, uint4(&f)[NP]) {
+            const uint4 x = *reinterpret_cast<const uint4*>(st + L::X_OFF + (16 * r + c) * 256 + 16 * ((4 * g + j) ^ c));
+            parts_of<NP>(x, d + 8 * j, f);
+          },
+          blk, total[r]);
+    slot = slot == DIST ? 0 : slot + 1;
   }
-  float* sums = reinterpret_cast<float*>(lds);
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(&ring[0][0][0]);
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -218,42 +299,51 @@ __global__ __launch_bounds__(512) void linear_rows_kernel(LinearArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) sums[((wave * NT + t) * 16 * RT + 16 * r + 4 * g + i) * 16 + c] = total[r][t][i];
   __syncthreads();
-  finish<NT>(a, sums, waves, 16 * RT, 1, n0);
+  finish<NT>(a, sums, L::WAVES, 16 * RT, 1, m0, rows, n0);
 }
 
 template <int NP, int NT>
-void launch_tiles(const LinearArgs& a, hipStream_t s) {
+void launch_staged(const LinearArgs& a, hipStream_t s) {
   const int nblk = a.K / kBlock;
-  const int R = a.M * NP;
   const unsigned grid = static_cast<unsigned>(a.N / (16 * NT));
-  if (R <= 16) {
-    const int waves = nblk >= 16 ? 16 : (nblk >= 8 ? 8 : 4);
-    const int iters = std::max(1, std::min((nblk + waves - 1) / waves, kStageBytes / (waves * R * 2 * kBlock)));
-    const size_t bytes = std::max(static_cast<size_t>(iters) * waves * R * 2 * kBlock, static_cast<size_t>(waves) * NT * 1024);
-    linear_staged_kernel<NP, NT><<<grid, 64 * waves, bytes, s>>>(a, iters);
-    return;
-  }
-  const int waves = nblk >= 8 ? 8 : 4;
-  const int rt = a.M <= 16 ? 1 : (a.M <= 32 ? 2 : 4);
-  const size_t bytes = static_cast<size_t>(waves) * NT * rt * 1024;
-  if (rt == 1) {
-    linear_rows_kernel<NP, NT, 1><<<grid, 64 * waves, bytes, s>>>(a);
-  } else if (rt == 2) {
-    linear_rows_kernel<NP, NT, 2><<<grid, 64 * waves, bytes, s>>>(a);
-  } else if constexpr (NT <= 2) {
-    linear_rows_kernel<NP, NT, 4><<<grid, 64 * waves, bytes, s>>>(a);
-  }
+  // sixteen waves where a CU has one workgroup (13824 -> 5120, one row: 13.5 us,
+  // eight 14.7), eight where it has two (5120 -> 15360: 12.4, sixteen 13.9)
+  const int waves = nblk >= 16 && grid <= 256 ? 16 : (nblk >= 8 ? 8 : 4);
+  const size_t bytes = std::max(static_cast<size_t>(a.M) * NP * a.K * 2, static_cast<size_t>(waves) * NT * 1024);
+  linear_staged_kernel<NP, NT><<<grid, 64 * waves, bytes, s>>>(a);
 }
 
+template <int NP, int NT, int RT>
+void launch_rows(const LinearArgs& a, hipStream_t s) {
+  const dim3 grid(a.N / (16 * NT), (a.M + 16 * RT - 1) / (16 * RT));
+  linear_rows_kernel<NP, NT, RT><<<grid, 64 * Ring<NP, NT, RT>::WAVES, 0, s>>>(a);
+}
+
+// Strips of 16 NT output channels: NT = 1 until the strips outnumber the CUs,
+// then wider ones, which share a workgroup's splitting of x~ (16 rows of
+// 13824 -> 5120: NT = 2 30 us, 1 53; 5120 -> 15360: NT = 4 17, 2 22).
 template <int NP>
 void launch_parts(const LinearArgs& a, hipStream_t s) {
   const int strips = a.N / 16;
-  if (strips <= 256) {
-    launch_tiles<NP, 1>(a, s);
-  } else if (strips <= 512 || a.M > 32) {
-    launch_tiles<NP, 2>(a, s);
+  if (a.M * NP <= 16 && static_cast<size_t>(a.M) * NP * a.K * 2 <= kStageBytes) {
+    if (strips <= 256)
+      launch_staged<NP, 1>(a, s);
+    else
+      launch_staged<NP, 2>(a, s);
+  } else if (a.M <= 16) {
+    if (strips <= 256)
+      launch_rows<NP, 1, 1>(a, s);
+    else if (strips <= 512)
+      launch_rows<NP, 2, 1>(a, s);
+    else
+      launch_rows<NP, 4, 1>(a, s);
   } else {
-    launch_tiles<NP, 4>(a, s);
+    if (strips <= 256)
+      launch_rows<NP, 1, 2>(a, s);
+    else if (strips <= 512)
+      launch_rows<NP, 2, 2>(a, s);
+    else
+      launch_rows<NP, 4, 2>(a, s);
   }
 }
 
