@@ -12,12 +12,17 @@ constexpr int kRopeThreads = 256;
 // the rotation pairs with each other (halves: chunk c and c + rot / 16), or
 // two adjacent chunks (adjacent pairs, and the values past rot).  So the
 // rotation needs no exchange between lanes, and the norm a sum over GL lanes.
-// The workgroup takes one token: its cos and sin stay in registers over the
-// heads.
+// A workgroup takes `per` heads of one token, whose cos and sin stay in
+// registers over the heads; the next head is loaded ahead.
 template <bool F16, bool INTER, int GL>
-__global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) {
-  const size_t t = flat_wg();
-  if (t >= static_cast<size_t>(a.T)) return;
+__global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, uint32_t parts, int per) {
+  constexpr int kGroups = kRopeThreads / GL;
+  const uint32_t wg = static_cast<uint32_t>(flat_wg());  // at most 2^24 tokens of 96 parts
+  const int heads = a.Hq + a.Hk + (a.v != nullptr ? a.Hk : 0);
+  if (wg >= static_cast<uint32_t>(a.T) * parts) return;
+  const uint32_t t32 = parts == 1 ? wg : wg / parts;
+  const size_t t = t32;
+  const int h0 = static_cast<int>(wg - t32 * parts) * per, end = min(h0 + per, heads);
   const int u = threadIdx.x % GL;  // pair of chunks
   const int D = a.D, rot = a.rot;
   const int pairs = D / 16, rpairs = rot / 16;
@@ -25,6 +30,17 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   const bool rotated = uc < rpairs;
   const int ca = INTER || !rotated ? 2 * uc : uc;
   const int cb = INTER || !rotated ? 2 * uc + 1 : uc + rpairs;
+
+  uint4 na = make_uint4(0, 0, 0, 0), nb = na;  // the next head's chunks
+  auto load = [&](int h) {
+    if (h >= end || u >= pairs) return;
+    const uint16_t* src = h < a.Hq          ? a.q + t * a.q_stride + static_cast<size_t>(h) * D
+                          : h < a.Hq + a.Hk ? a.k + t * a.k_stride + static_cast<size_t>(h - a.Hq) * D
+                                            : a.v + t * a.v_stride + static_cast<size_t>(h - a.Hq - a.Hk) * D;
+    na = *reinterpret_cast<const uint4*>(src + 8 * ca);
+    nb = *reinterpret_cast<const uint4*>(src + 8 * cb);
+  };
+  load(h0 + threadIdx.x / GL);
 
   float c[8], n[8];
   if (rot > 0) {
@@ -42,20 +58,13 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   const size_t page = cached ? slot >> a.page_shift : 0;
   const int in_page = slot & ((1 << a.page_shift) - 1);
 
-  const int heads = a.Hq + a.Hk + (a.v != nullptr ? a.Hk : 0);
-  for (int h0 = 0; h0 < heads; h0 += kRopeThreads / GL) {
-    const int h = h0 + threadIdx.x / GL;
-    const bool live = h < heads && u < pairs;
+  for (int hb = h0; hb < end; hb += kGroups) {
+    const int h = hb + threadIdx.x / GL;
+    const bool live = h < end && u < pairs;
     const int kind = h < a.Hq ? 0 : (h < a.Hq + a.Hk ? 1 : 2);
     const int hh = kind == 0 ? h : (kind == 1 ? h - a.Hq : h - a.Hq - a.Hk);
-    const uint16_t* src = kind == 0   ? a.q + t * a.q_stride + static_cast<size_t>(hh) * D
-                          : kind == 1 ? a.k + t * a.k_stride + static_cast<size_t>(hh) * D
-                                      : a.v + t * a.v_stride + static_cast<size_t>(hh) * D;
-    uint4 ra = make_uint4(0, 0, 0, 0), rb = ra;
-    if (live) {
-      ra = *reinterpret_cast<const uint4*>(src + 8 * ca);
-      rb = *reinterpret_cast<const uint4*>(src + 8 * cb);
-    }
+    const uint4 ra = na, rb = nb;
+    if (hb + kGroups < end) load(h + kGroups);
     const size_t row = ((page * a.Hk + hh) << a.page_shift) + in_page;
     if (kind == 2) {
       if (live && cached) {
@@ -121,15 +130,26 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a) 
   }
 }
 
+template <bool F16, bool INTER, int GL>
+void launch_groups(const RopeArgs& a, hipStream_t s) {
+  constexpr int kGroups = kRopeThreads / GL;
+  const int heads = a.Hq + a.Hk + (a.v != nullptr ? a.Hk : 0);
+  const int rounds = (heads + kGroups - 1) / kGroups;
+  // few tokens: their heads over more workgroups, a round each (8 tokens of 120
+  // heads: 6.8 us in four rounds, 5.9; from 512 on the parts only repeat cos and sin)
+  const uint32_t parts = a.T < 512 ? rounds : 1;
+  const int per = (rounds + static_cast<int>(parts) - 1) / static_cast<int>(parts) * kGroups;
+  qk_norm_rope_kernel<F16, INTER, GL><<<wg_grid(static_cast<size_t>(a.T) * parts), kRopeThreads, 0, s>>>(a, parts, per);
+}
+
 template <bool F16, bool INTER>
 void launch_head_width(const RopeArgs& a, hipStream_t s) {
-  const dim3 grid = wg_grid(a.T);
   if (a.D <= 64) {
-    qk_norm_rope_kernel<F16, INTER, 4><<<grid, kRopeThreads, 0, s>>>(a);
+    launch_groups<F16, INTER, 4>(a, s);
   } else if (a.D <= 128) {
-    qk_norm_rope_kernel<F16, INTER, 8><<<grid, kRopeThreads, 0, s>>>(a);
+    launch_groups<F16, INTER, 8>(a, s);
   } else {
-    qk_norm_rope_kernel<F16, INTER, 16><<<grid, kRopeThreads, 0, s>>>(a);
+    launch_groups<F16, INTER, 16>(a, s);
   }
 }
 
