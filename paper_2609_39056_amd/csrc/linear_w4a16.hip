@@ -192,22 +192,23 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
 // registers as it takes the fragments.  The copies go along the rows, four
 // rows of 256 bytes (16 of 64) per instruction; loads in the fragments' own
 // layout touch a line with every lane, and those kept the address unit busy for
-// the whole kernel (16 rows of 13824 -> 5120 channels: 23 us without a
-// channel scaling, 33 with one).  Rows past M repeat the last one and are not
-// stored.  A wave reads only what it copied: the loop has no barriers.
+// the whole kernel (16 rows of 13824 -> 5120 without a channel scaling: 22.8 us,
+// now 13.8).  A wave reads only what it copied: the loop has no barriers.  More
+// waves with no block ahead hide the latency better than fewer with one (16
+// rows of 13824 -> 5120, scaled, fp32 out: twelve waves 30.2 us, eight with a
+// block ahead 31.1; 64 rows of 5120 -> 13824: eight waves 43.2, four 48.6), where
+// registers leave room for them.  What is left there is the splitting of x~:
+// 7.5 vector operations a value in every workgroup.
 template <int NP, int NT, int RT>
 struct Ring {
   static constexpr int X = RT * 16 * 2 * kBlock;    // row r, 16-byte chunk k at r * 256 + 16 * (k ^ (r & 15))
   static constexpr int W = NT * 16 * (kBlock / 2);  // channel n, chunk k at n * 64 + 16 * (k ^ ((n >> 2) & 3))
-  static constexpr int X_OFF = 0, W_OFF = X, S_OFF = X + W, D_OFF = S_OFF + 256;
+  static constexpr int W_OFF = X, S_OFF = X + W, D_OFF = S_OFF + 256;
   static constexpr int SLOT = D_OFF + (NP > 1 ? 4 * kBlock : 0);
   static constexpr int COPIES = RT * 4 + NT + 1 + (NP > 1 ? 2 : 0);
-  // blocks in the ring and waves of a workgroup.  Twelve waves without a block
-  // ahead hide the latency better than eight with one (16 rows of 13824 -> 5120,
-  // scaled, fp32: 30.2 and 31.1 us; sixteen spill registers, 29.3 to 30.2); the
-  // wider strips of NT = 4 take eight (5120 -> 15360: 17.1, 19 with twelve)
-  static constexpr int SLOTS = RT == 1 && NT <= 2 ? 1 : 2;
-  static constexpr int WAVES = RT == 1 ? (NT <= 2 ? 12 : 8) : 4;
+  static constexpr bool WIDE = RT == 2 && NT == 4 && NP == 3;  // the most registers
+  static constexpr int SLOTS = (RT == 1 && NT == 4) || WIDE ? 2 : 1;
+  static constexpr int WAVES = WIDE ? 4 : RT == 1 && NT <= 2 ? 12 : 8;
   static_assert(WAVES * SLOTS * SLOT <= 160 * 1024, "the rings fit in the LDS");
   static_assert(NT * RT * 1024 <= SLOTS * SLOT, "the waves' sums fit in the rings");
 };
@@ -242,7 +243,7 @@ __global__ __launch_bounds__((64 * Ring<NP, NT, RT>::WAVES)) void linear_rows_ke
     for (int t = 0; t < NT; ++t) dma<16>(qw + b * (kBlock / 2), woff[t], at + L::W_OFF + t * 1024);
     dma<4>(a.w_scale + static_cast<size_t>((b * kBlock) / a.w_group) * a.N + n0, soff, at + L::S_OFF);
 #pragma unroll
-    for (int i = 0; i < RT * 4; ++i) dma<16>(xs + b * kBlock, xoff[i], at + L::X_OFF + i * 1024);
+    for (int i = 0; i < RT * 4; ++i) dma<16>(xs + b * kBlock, xoff[i], at + i * 1024);
     if constexpr (NP > 1) {
       dma<4>(a.dinv + b * kBlock, 4 * lane, at + L::D_OFF);
       dma<4>(a.dinv + b * kBlock + 64, 4 * lane, at + L::D_OFF + 256);
@@ -262,10 +263,7 @@ __global__ __launch_bounds__((64 * Ring<NP, NT, RT>::WAVES)) void linear_rows_ke
   for (int b = wave; b < nblk; b += L::WAVES) {
     // the slot that is filled next was read in the last pass: its reads are done
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (DIST == 0) {
-      copy(b, 0);
-      wait_vm<0>();
-    } else if (b + DIST * L::WAVES < nblk) {
+    if (b + DIST * L::WAVES < nblk) {
       copy(b + DIST * L::WAVES, slot == 0 ? DIST : slot - 1);
       wait_vm<DIST * L::COPIES>();
     } else {
@@ -284,7 +282,7 @@ __global__ __launch_bounds__((64 * Ring<NP, NT, RT>::WAVES)) void linear_rows_ke
     for (int r = 0; r < RT; ++r)
       add_block<NT, NP>(
           [&](int j, uint4(&f)[NP]) {
-            const uint4 x = *reinterpret_cast<const uint4*>(st + L::X_OFF + (16 * r + c) * 256 + 16 * ((4 * g + j) ^ c));
+            const uint4 x = *reinterpret_cast<const uint4*>(st + (16 * r + c) * 256 + 16 * ((4 * g + j) ^ c));
             parts_of<NP>(x, d + 8 * j, f);
           },
           blk, total[r]);
