@@ -7,7 +7,6 @@
 namespace sq {
 namespace {
 
-constexpr int kWaves = 4;    // of a workgroup
 constexpr int kTile = kAttnTile, kQTile = kAttnQTile;  // kQTile: the columns of a 16 x 16 matrix-core tile
 constexpr int kMinPage = 8;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -62,8 +61,9 @@ __device__ __forceinline__ float2* part_stats(const AttnArgs& a, const AttnSplit
   return reinterpret_cast<float2*>(a.part + static_cast<size_t>(a.R) * a.Hq * sp.count * a.D);
 }
 
-template <bool F16, int D, int NP>
-__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
+// W waves take a chunk.
+template <bool F16, int D, int NP, int W>
+__global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
   constexpr int KF = D / 32;  // fragments of a key row
   // a lane's part of a value row: E dimensions, E0 c .. of the first 16 E0 and
   // E1 c .. of the rest, so that a load covers whole lines across the lanes
@@ -72,13 +72,13 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
   // The next tile's keys are loaded once this tile's scores are formed, its
   // values after the products (3 to 4 % at head dimension 128); at 256 the
   // registers that takes leave one workgroup per CU (58 us, without 50).
-  constexpr bool kAhead = D < 256;
-  constexpr int kPages = kAttnWhole / kMinPage + 1;  // pages of a chunk: one for each of as many threads
-  static_assert(kPages <= 64 * kWaves, "one table entry per thread");
+  constexpr bool kAhead = D < 256 && W > 1;
+  constexpr int kPages = (W == 1 ? kAttnLone : kAttnWhole) / kMinPage + 1;  // of a chunk: one for each of as many threads
+  static_assert(kPages <= 64 * W, "one table entry per thread");
   constexpr float kShift = F16 ? 11.0f : 0.0f;
   constexpr float kSlack = F16 ? 4.0f : 8.0f;
   __shared__ int32_t pages[kPages];
-  __shared__ float s_m[kWaves][kQTile], s_l[kWaves][kQTile], s_o[kWaves][kQTile][D + 4];
+  __shared__ float s_m[W][kQTile], s_l[W][kQTile], s_o[W][kQTile][D + 4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -139,10 +139,17 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
   uint4 k[2][KF];
   uint32_t v[8][EW];
   int kp[2], vp[2];
+  // Tokens outside [first, end) are not loaded: their lanes repeat the nearest
+  // row inside (a short history would otherwise cost a whole tile of 16 KB).
+  auto inside = [&](int b) { return b >= first && b + kTile <= end; };
+  auto load_v_row = [&](const uint16_t* p, uint32_t* w) {
+    load_words<E0 / 2>(p + E0 * c, w);
+    if constexpr (E1 > 0) load_words<E1 / 2>(p + 16 * E0 + E1 * c, w + E0 / 2);
+  };
   auto load_k = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int tok = b + 16 * i + c;
+      const int tok = max(first, min(b + 16 * i + c, end - 1));
       kp[i] = page_of(tok);
       const uint16_t* p = a.k + row_of(kp[i], tok) * D + 8 * g;
 #pragma unroll
@@ -152,13 +159,15 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
   auto load_v = [&](int b) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int tok = b + 16 * i + 4 * g;
-      vp[i] = page_of(tok);
-      const uint16_t* p = a.v + row_of(vp[i], tok) * D;
+      const int tok = b + 16 * i + 4 * g, tc = max(first, min(tok, end - 1));
+      vp[i] = page_of(tc);
+      const uint16_t* p = a.v + row_of(vp[i], tc) * D;
+      if (inside(b)) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        load_words<E0 / 2>(p + x * D + E0 * c, v[4 * i + x]);
-        if constexpr (E1 > 0) load_words<E1 / 2>(p + x * D + 16 * E0 + E1 * c, v[4 * i + x] + E0 / 2);
+        for (int x = 0; x < 4; ++x) load_v_row(p + x * D, v[4 * i + x]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) load_v_row(p + max(0, min(tok + x, end - 1) - tc) * D, v[4 * i + x]);
       }
     }
   };
@@ -166,7 +175,7 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
     load_k(begin + wave * kTile);
     load_v(begin + wave * kTile);
   }
-  for (int t = wave; t < tiles; t += kWaves) {
+  for (int t = wave; t < tiles; t += W) {
     const int b = begin + t * kTile;
     if (!kAhead) {
       load_k(b);
@@ -182,8 +191,8 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
     float f[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = s[i / 4][i % 4] * scale;
-    const bool whole_tile = b >= first && b + kTile <= end && __all(kp[0] >= 0 && kp[1] >= 0);
-    if (kAhead && t + kWaves < tiles) load_k(b + kWaves * kTile);
+    const bool whole_tile = inside(b) && __all(kp[0] >= 0 && kp[1] >= 0);
+    if (kAhead && t + W < tiles) load_k(b + W * kTile);
     if (!whole_tile) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
 #pragma unroll
       for (int u = 0; u < NP; ++u) o[e] = mfma<F16>(vt, make_uint4(p[u][0], p[u][1], p[u][2], p[u][3]), o[e]);
     }
-    if (kAhead && t + kWaves < tiles) load_v(b + kWaves * kTile);
+    if (kAhead && t + W < tiles) load_v(b + W * kTile);
   }
 
   // the waves' parts: column c, and the dimensions that lane 4 g + x loaded
@@ -244,14 +253,14 @@ __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void attn_kernel(Att
     for (int x = 0; x < 4; ++x)
       if (c < gq) s_o[wave][c][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[e][x];
   __syncthreads();
-  for (int i = threadIdx.x; i < gq * D; i += 64 * kWaves) {
+  for (int i = threadIdx.x; i < gq * D; i += 64 * W) {
     const int qh = i / D, d = i % D;
     float M = s_m[0][qh];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][qh]);
+    for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][qh]);
     float y = 0.0f, L = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float al = __builtin_amdgcn_exp2f(s_m[w][qh] - M);
       L = __builtin_fmaf(s_l[w][qh], al, L);
       y = __builtin_fmaf(s_o[w][qh][d], al, y);
@@ -380,17 +389,27 @@ __global__ __launch_bounds__(THREADS) void attn_join_kernel(AttnArgs a, AttnSpli
   if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
-template <bool F16, int NP>
+template <bool F16, int NP, int W>
 void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
   const int qt = (a.Hq / a.Hk + kQTile - 1) / kQTile;
   const dim3 grid(static_cast<unsigned>(a.Hk * qt * sp.count), static_cast<unsigned>(a.R));
   switch (a.D) {
-    case 64: attn_kernel<F16, 64, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
-    case 96: attn_kernel<F16, 96, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
-    case 128: attn_kernel<F16, 128, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
-    case 192: attn_kernel<F16, 192, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
-    default: attn_kernel<F16, 256, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp, qt); break;
+    case 64: attn_kernel<F16, 64, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
+    case 96: attn_kernel<F16, 96, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
+    case 128: attn_kernel<F16, 128, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
+    case 192: attn_kernel<F16, 192, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
+    default: attn_kernel<F16, 256, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
   }
+}
+
+template <int W>
+void launch_waves(const AttnArgs& a, const AttnSplit& sp, bool f16, hipStream_t s) {
+  if (f16)
+    launch_dim<true, 2, W>(a, sp, s);
+  else if (a.out_dtype == SQ_OUT_F32)
+    launch_dim<false, 3, W>(a, sp, s);
+  else
+    launch_dim<false, 2, W>(a, sp, s);
 }
 
 }  // namespace
@@ -401,15 +420,14 @@ size_t attn_partial_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t 
 
 hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
   const int64_t heads = attn_heads(a.R, a.Hq, a.Hk);
-  const AttnSplit sp = attn_split(heads, attn_span(a.max_kv_len, a.window));
+  const int64_t span = attn_span(a.max_kv_len, a.window);
+  const AttnSplit sp = attn_split(heads, span);
   if (attn_part_bytes(a.R, a.Hq, a.D, sp.count) > a.part_bytes) return hipErrorInvalidValue;
   if (heads / a.R * sp.count >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
-  if (f16)
-    launch_dim<true, 2>(a, sp, s);
-  else if (a.out_dtype == SQ_OUT_F32)
-    launch_dim<false, 3>(a, sp, s);
+  if (attn_lone(heads, span))
+    launch_waves<1>(a, sp, f16, s);
   else
-    launch_dim<false, 2>(a, sp, s);
+    launch_waves<4>(a, sp, f16, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.count == 1) return e;
   const dim3 rows = wg_grid(static_cast<size_t>(a.R) * a.Hq * (a.D / 32));

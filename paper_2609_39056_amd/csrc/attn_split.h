@@ -19,6 +19,7 @@
 namespace sq {
 
 constexpr int32_t kAttnWhole = 1280;      // the longest span that is ever left whole
+constexpr int32_t kAttnLone = 64;         // the longest span that one wave ever takes alone
 constexpr int32_t kAttnQTile = 16;        // query heads of a workgroup
 constexpr int32_t kAttnTile = 32;         // tokens a wave takes at a time; spans start at a multiple of it
 
@@ -33,6 +34,11 @@ inline int64_t attn_heads(int32_t R, int32_t Hq, int32_t Hk) {
 }
 inline int64_t attn_wanted(int64_t heads) { return std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads)); }
 inline bool attn_whole(int64_t heads, int64_t span) { return span <= (heads >= 192 ? kAttnWhole : 384); }
+// Whether a workgroup is a single wave: for one tile, and for two where the
+// heads fill the CUs several times over (2160 heads of up to 24 tokens 9.3 us,
+// with four waves 14.5; 4000 of 64 17.7 and 26.2; but 160 of 64 7.4 and 6.5, and
+// 800 of 128 13.0 and 11.0).
+inline bool attn_lone(int64_t heads, int64_t span) { return span <= (heads > 768 ? kAttnLone : kAttnTile); }
 constexpr int64_t kAttnLeastShort = 128, kAttnLeast = 256, kAttnMost = 512, kAttnMostLong = 1024;
 constexpr int64_t kAttnShort = 4096, kAttnLong = 65536;
 

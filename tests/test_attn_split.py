@@ -17,8 +17,8 @@ int main() {
   while (scanf("%d %d %d %d %d", &R, &Hq, &Hk, &longest, &window) == 5) {
     const long long heads = attn_heads(R, Hq, Hk), span = attn_span(longest, window);
     const AttnSplit s = attn_split(heads, span);
-    printf("%lld %lld %d %d %lld %zu\\n", heads, span, s.chunk, s.count, (long long)attn_most_splits(heads, longest),
-           attn_part_bytes(R, Hq, 128, attn_most_splits(heads, longest)));
+    printf("%lld %lld %d %d %lld %zu %d\\n", heads, span, s.chunk, s.count, (long long)attn_most_splits(heads, longest),
+           attn_part_bytes(R, Hq, 128, attn_most_splits(heads, longest)), attn_lone(heads, span));
   }
 }
 """
@@ -56,7 +56,7 @@ def cases():
 
 def test_every_split_covers_its_span_and_fits_the_workspace(split):
     asked = list(cases())
-    for (R, Hq, Hk, longest, window), (heads, span, chunk, count, most, nbytes) in zip(asked, split(asked)):
+    for (R, Hq, Hk, longest, window), (heads, span, chunk, count, most, nbytes, lone) in zip(asked, split(asked)):
         what = (R, Hq, Hk, longest, window)
         assert heads == R * Hk * -(-(Hq // Hk) // 16), what
         # any window [n - window, n) from a multiple of 32 on, any n up to the longest
@@ -69,3 +69,5 @@ def test_every_split_covers_its_span_and_fits_the_workspace(split):
         assert nbytes == (0 if most == 1 else R * Hq * most * 130 * 4), what
         if count == 1 and span > 0:
             assert chunk >= span, what
+        # a lone wave has the whole span, whose pages of 8 tokens are no more than its lanes
+        assert not lone or (count == 1 and span <= 64), what
