@@ -61,6 +61,21 @@ __device__ __forceinline__ float2* part_stats(const AttnArgs& a, const AttnSplit
   return reinterpret_cast<float2*>(a.part + static_cast<size_t>(a.R) * a.Hq * sp.count * a.D);
 }
 
+__device__ __forceinline__ void add_scaled(float4& y, const float4& v, float al) {
+  y.x = __builtin_fmaf(v.x, al, y.x);
+  y.y = __builtin_fmaf(v.y, al, y.y);
+  y.z = __builtin_fmaf(v.z, al, y.z);
+  y.w = __builtin_fmaf(v.w, al, y.w);
+}
+
+// Four outputs of a query head, and its lse once, from the maximum (in units
+// of log 2), the sum and the weighted values.  An empty sum gives 0.
+__device__ __forceinline__ void finish_row(const AttnArgs& a, size_t row, int d4, float M, float L, const float4& y) {
+  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  store_out4(a.out, row * (a.D / 4) + d4, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), a.out_dtype);
+  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+}
+
 // W waves take a chunk.
 template <bool F16, int D, int NP, int W>
 __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
@@ -253,26 +268,26 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
     for (int x = 0; x < 4; ++x)
       if (c < gq) s_o[wave][c][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[e][x];
   __syncthreads();
-  for (int i = threadIdx.x; i < gq * D; i += 64 * W) {
-    const int qh = i / D, d = i % D;
+  for (int i = threadIdx.x; i < gq * (D / 4); i += 64 * W) {
+    const int qh = i / (D / 4), d4 = i % (D / 4);
     float M = s_m[0][qh];
 #pragma unroll
     for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][qh]);
-    float y = 0.0f, L = 0.0f;
+    float4 y = make_float4(0, 0, 0, 0);
+    float L = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float al = __builtin_amdgcn_exp2f(s_m[w][qh] - M);
       L = __builtin_fmaf(s_l[w][qh], al, L);
-      y = __builtin_fmaf(s_o[w][qh][d], al, y);
+      add_scaled(y, *reinterpret_cast<const float4*>(&s_o[w][qh][4 * d4]), al);
     }
     const size_t row = static_cast<size_t>(r) * a.Hq + h0 + qh;
     if (whole) {
-      store_out(a.out, row * D + d, L > 0.0f ? y / L : 0.0f, a.out_dtype);
-      if (d == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+      finish_row(a, row, d4, M, L, y);
     } else {
       const size_t part = row * sp.count + split;
-      a.part[part * D + d] = y;
-      if (d == 0) part_stats(a, sp)[part] = make_float2(M, L);
+      reinterpret_cast<float4*>(a.part)[part * (D / 4) + d4] = y;
+      if (d4 == 0) part_stats(a, sp)[part] = make_float2(M, L);
     }
   }
 }
@@ -291,7 +306,8 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnSpli
   const int d4 = static_cast<int>(i % D4);
   const float4* po = reinterpret_cast<const float4*>(a.part) + row * sp.count * D4 + d4;
   const float2* pm = part_stats(a, sp) + row * sp.count;
-  float M = kLowest, L = 0.0f, v[4] = {0, 0, 0, 0};
+  float M = kLowest, L = 0.0f;
+  float4 v = make_float4(0, 0, 0, 0);
   constexpr int kAhead = 8;  // parts whose loads are in flight together
   for (int s0 = 0; s0 < count; s0 += kAhead) {
     float2 ml[kAhead];
@@ -309,21 +325,15 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnArgs a, AttnSpli
     const float was = __builtin_amdgcn_exp2f(M - mn);
     M = mn;
     L *= was;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v[x] *= was;
+    v = make_float4(v.x * was, v.y * was, v.z * was, v.w * was);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const float al = s0 + u < count ? __builtin_amdgcn_exp2f(ml[u].x - mn) : 0.0f;
       L = __builtin_fmaf(ml[u].y, al, L);
-      v[0] = __builtin_fmaf(o[u].x, al, v[0]);
-      v[1] = __builtin_fmaf(o[u].y, al, v[1]);
-      v[2] = __builtin_fmaf(o[u].z, al, v[2]);
-      v[3] = __builtin_fmaf(o[u].w, al, v[3]);
+      add_scaled(v, o[u], al);
     }
   }
-#pragma unroll
-  for (int x = 0; x < 4; ++x) store_out(a.out, row * a.D + 4 * d4 + x, L > 0.0f ? v[x] / L : 0.0f, a.out_dtype);
-  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+  finish_row(a, row, d4, M, L, v);
 }
 
 // Joins the parts of a split history, many of them: a workgroup takes 32 dimensions of one
@@ -354,39 +364,33 @@ __global__ __launch_bounds__(THREADS) void attn_join_kernel(AttnArgs a, AttnSpli
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWavesHere; ++w) M = fmaxf(M, s_max[w]);
-  float v[5] = {0, 0, 0, 0, 0};
+  float4 v = make_float4(0, 0, 0, 0);
+  float L = 0.0f;
   for (int s = tid / 8; s < count; s += kParts) {
     const float2 ml = pm[s];
-    const float4 o = po[static_cast<size_t>(s) * D4];
     const float al = __builtin_amdgcn_exp2f(ml.x - M);
-    v[0] = __builtin_fmaf(o.x, al, v[0]);
-    v[1] = __builtin_fmaf(o.y, al, v[1]);
-    v[2] = __builtin_fmaf(o.z, al, v[2]);
-    v[3] = __builtin_fmaf(o.w, al, v[3]);
-    v[4] = __builtin_fmaf(ml.y, al, v[4]);
+    add_scaled(v, po[static_cast<size_t>(s) * D4], al);
+    L = __builtin_fmaf(ml.y, al, L);
   }
 #pragma unroll
-  for (int o = 8; o < 64; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 5; ++i) v[i] += __shfl_xor(v[i], o, 64);
+  for (int o = 8; o < 64; o <<= 1) {
+    v.x += __shfl_xor(v.x, o, 64);
+    v.y += __shfl_xor(v.y, o, 64);
+    v.z += __shfl_xor(v.z, o, 64);
+    v.w += __shfl_xor(v.w, o, 64);
+    L += __shfl_xor(L, o, 64);
+  }
   if (lane < 8) {
-    s_sum[wave][lane] = make_float4(v[0], v[1], v[2], v[3]);
-    if (lane == 0) s_l[wave] = v[4];
+    s_sum[wave][lane] = v;
+    if (lane == 0) s_l[wave] = L;
   }
   __syncthreads();
   if (tid >= 8) return;
   for (int w = 1; w < kWavesHere; ++w) {
-    const float4 o = s_sum[w][tid];
-    v[0] += o.x;
-    v[1] += o.y;
-    v[2] += o.z;
-    v[3] += o.w;
-    v[4] += s_l[w];
+    add_scaled(v, s_sum[w][tid], 1.0f);
+    L += s_l[w];
   }
-  const float L = v[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) store_out(a.out, row * a.D + 4 * d4 + i, L > 0.0f ? v[i] / L : 0.0f, a.out_dtype);
-  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+  finish_row(a, row, d4, M, L, v);
 }
 
 template <bool F16, int NP, int W>

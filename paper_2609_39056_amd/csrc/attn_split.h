@@ -3,9 +3,10 @@
 // A workgroup costs about 5 us from its launch to its last store (three
 // dependent loads, the join of its waves) and 1.2 us per 128 tokens; a split
 // adds a second kernel, 3 to 6 us.  So short spans stay whole: up to 384
-// tokens, or up to 1280 where the (request, head) pairs alone fill the CUs (768
-// heads with 1055 tokens: 38 us whole, 42 in five parts, 47 in two; 1024 heads
-// with up to 1000: 55 whole, 68 in two).  Longer ones aim at 2048 workgroups in
+// tokens, up to 640 from 192 (request, head) pairs on (192 with 531 tokens: 22 us
+// whole, 26 in parts), and up to 1280 where the pairs alone fill the CUs (768
+// with 1055 tokens: 38 us whole, 42 in five parts, 47 in two; 1024 with up to
+// 1000: 55 whole, 68 in two).  Longer ones aim at 2048 workgroups in
 // all, eight per CU, so that ragged batches even out: 512 heads with 1024 to
 // 8192 tokens take 176 us in chunks of 512, 193 in 1024, 212 in 1152.  Spans
 // past 65536 may take chunks of 1024 (two histories of 131072, 8 heads: 136 us,
@@ -33,7 +34,7 @@ inline int64_t attn_heads(int32_t R, int32_t Hq, int32_t Hk) {
   return static_cast<int64_t>(R) * Hk * ((Hq / Hk + kAttnQTile - 1) / kAttnQTile);
 }
 inline int64_t attn_wanted(int64_t heads) { return std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads)); }
-inline bool attn_whole(int64_t heads, int64_t span) { return span <= (heads >= 192 ? kAttnWhole : 384); }
+inline bool attn_whole(int64_t heads, int64_t span) { return span <= (heads >= 512 ? kAttnWhole : heads >= 192 ? 640 : 384); }
 // Whether a workgroup is a single wave: for one tile, and for two where the
 // heads fill the CUs several times over (2160 heads of up to 24 tokens 9.3 us,
 // with four waves 14.5; 4000 of 64 17.7 and 26.2; but 160 of 64 7.4 and 6.5, and

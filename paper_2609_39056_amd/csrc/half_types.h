@@ -53,5 +53,16 @@ __device__ __forceinline__ void store_out(void* y, size_t i, float v, int32_t ou
   }
 }
 
+// Four of them from index 4 i on.
+__device__ __forceinline__ void store_out4(void* y, size_t i, const float4& v, int32_t out_dtype) {
+  if (out_dtype == SQ_OUT_F32) {
+    static_cast<float4*>(y)[i] = v;
+  } else if (out_dtype == SQ_OUT_BF16) {
+    static_cast<uint2*>(y)[i] = make_uint2(to_half2<false>(v.x, v.y), to_half2<false>(v.z, v.w));
+  } else {
+    static_cast<uint2*>(y)[i] = make_uint2(to_half2<true>(v.x, v.y), to_half2<true>(v.z, v.w));
+  }
+}
+
 }  // namespace
 }  // namespace sq
