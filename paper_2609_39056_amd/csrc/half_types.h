@@ -23,9 +23,15 @@ __device__ __forceinline__ uint32_t to_half(float v) {
   if constexpr (F16) return f32_to_f16(v);
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
+// Both halves with one conversion.
 template <bool F16>
 __device__ __forceinline__ uint32_t to_half2(float lo, float hi) {
-  return to_half<F16>(lo) | (to_half<F16>(hi) << 16);
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+  const f32x2_t v = {lo, hi};
+  if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
 // 8 values of 16 bits <-> 8 floats

@@ -25,7 +25,6 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 128;              // channels of a block
-constexpr int kStageBytes = 64 << 10;    // LDS for staged activations
 
 __device__ __forceinline__ v4f mfma(const uint4& x, const uint4& w, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w), c, 0, 0, 0);
@@ -139,10 +138,11 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const float* sums, i
   }
 }
 
-// Few rows (M * NP <= 16, all of x~ in 64 KB): the parts of x~ are rows of one
-// matrix-core tile.  The workgroup stages them in LDS, in 16-byte pieces
-// ((block * 4 + j) * 4 + g) * R + row, so every x~ is split once per workgroup
-// and only as many rows as there are; the wave's next block is loaded ahead.
+// A row or a few with a channel scaling: the parts of x~ are rows of one
+// matrix-core tile.  The workgroup stages all of them in LDS, in 16-byte pieces
+// ((block * 4 + j) * 4 + g) * R + row, so that only the rows there are get split,
+// by all its lanes (one row of 13824 -> 5120: 13.4 us, with the kernel below
+// 21.0); the wave's next block is loaded ahead.
 template <int NP, int NT>
 __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -186,19 +186,19 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
   finish<NT>(a, sums, waves, 16, NP, 0, a.M, n0);
 }
 
-// More rows: RT tiles of 16 rows.  Each wave copies its blocks (activation
-// rows, weights, weight steps and the channel scaling) by direct global -> LDS
-// loads into a ring of its own, SLOTS - 1 blocks ahead, and splits x~ in
-// registers as it takes the fragments.  The copies go along the rows, four
-// rows of 256 bytes (16 of 64) per instruction; loads in the fragments' own
-// layout touch a line with every lane, and those kept the address unit busy for
-// the whole kernel (16 rows of 13824 -> 5120 without a channel scaling: 22.8 us,
-// now 13.8).  A wave reads only what it copied: the loop has no barriers.  More
-// waves with no block ahead hide the latency better than fewer with one (16
-// rows of 13824 -> 5120, scaled, fp32 out: twelve waves 30.2 us, eight with a
-// block ahead 31.1; 64 rows of 5120 -> 13824: eight waves 43.2, four 48.6), where
-// registers leave room for them.  What is left there is the splitting of x~:
-// 7.5 vector operations a value in every workgroup.
+// The rest: RT tiles of 16 rows.  Each wave copies its blocks (activation rows,
+// weights, weight steps and the channel scaling) by direct global -> LDS loads
+// into a ring of its own, SLOTS - 1 blocks ahead, and splits x~ in registers as
+// it takes the fragments.  The copies go along the rows, four rows of 256
+// bytes (16 of 64) per instruction; loads in the fragments' own layout touch a
+// line with every lane, and those kept the address unit busy for the whole
+// kernel (16 rows of 13824 -> 5120 without a channel scaling: 22.8 us, now 13.8).
+// A wave reads only what it copied: the loop has no barriers.  With two row
+// tiles eight waves and no block ahead do better than four with one (64 rows of
+// 5120 -> 13824: 38.4 us, 42.6), where registers leave room for them.  With a
+// scaling and 16 rows what is left is the splitting of x~ in every workgroup, 7.5
+// vector operations a value (13824 -> 5120, fp32 out: 25 us, vector units 80 %
+// busy; 13.8 without).
 template <int NP, int NT, int RT>
 struct Ring {
   static constexpr int X = RT * 16 * 2 * kBlock;    // row r, 16-byte chunk k at r * 256 + 16 * (k ^ (r & 15))
@@ -207,8 +207,8 @@ struct Ring {
   static constexpr int SLOT = D_OFF + (NP > 1 ? 4 * kBlock : 0);
   static constexpr int COPIES = RT * 4 + NT + 1 + (NP > 1 ? 2 : 0);
   static constexpr bool WIDE = RT == 2 && NT == 4 && NP == 3;  // the most registers
-  static constexpr int SLOTS = (RT == 1 && NT == 4) || WIDE ? 2 : 1;
-  static constexpr int WAVES = WIDE ? 4 : RT == 1 && NT <= 2 ? 12 : 8;
+  static constexpr int SLOTS = RT == 1 || WIDE ? 2 : 1;
+  static constexpr int WAVES = WIDE ? 4 : 8;
   static_assert(WAVES * SLOTS * SLOT <= 160 * 1024, "the rings fit in the LDS");
   static_assert(NT * RT * 1024 <= SLOTS * SLOT, "the waves' sums fit in the rings");
 };
@@ -304,8 +304,8 @@ template <int NP, int NT>
 void launch_staged(const LinearArgs& a, hipStream_t s) {
   const int nblk = a.K / kBlock;
   const unsigned grid = static_cast<unsigned>(a.N / (16 * NT));
-  // sixteen waves where a CU has one workgroup (13824 -> 5120, one row: 13.5 us,
-  // eight 14.7), eight where it has two (5120 -> 15360: 12.4, sixteen 13.9)
+  // sixteen waves where a CU has one workgroup (13824 -> 5120, one row: 13.4 us,
+  // eight 14.2), eight where it has two (5120 -> 15360: 12.2, sixteen 13.8)
   const int waves = nblk >= 16 && grid <= 256 ? 16 : (nblk >= 8 ? 8 : 4);
   const size_t bytes = std::max(static_cast<size_t>(a.M) * NP * a.K * 2, static_cast<size_t>(waves) * NT * 1024);
   linear_staged_kernel<NP, NT><<<grid, 64 * waves, bytes, s>>>(a);
@@ -317,17 +317,29 @@ void launch_rows(const LinearArgs& a, hipStream_t s) {
   linear_rows_kernel<NP, NT, RT><<<grid, 64 * Ring<NP, NT, RT>::WAVES, 0, s>>>(a);
 }
 
+// Whether the staged kernel takes the layer: up to six rows of parts (two rows
+// of 5120 -> 5120: 9.1 us, 11.0 by the other; eight rows of 2048 -> 8192 8.6, 7.2),
+// as far as the LDS holds them beside a second workgroup where there is one (three
+// rows of 11264 -> 9792, 135 KB: 27.3, 23.3 by the other).
+template <int NP>
+bool staged(const LinearArgs& a) {
+  const size_t bytes = static_cast<size_t>(a.M) * NP * a.K * 2;
+  return NP > 1 && a.M * NP <= 6 && bytes <= (a.N / 16 <= 512 ? 144 << 10 : 80 << 10);
+}
+
 // Strips of 16 NT output channels: NT = 1 until the strips outnumber the CUs,
 // then wider ones, which share a workgroup's splitting of x~ (16 rows of
-// 13824 -> 5120: NT = 2 30 us, 1 53; 5120 -> 15360: NT = 4 17, 2 22).
+// 13824 -> 5120, fp32 out: NT = 2 25 us, 1 40; 5120 -> 15360: NT = 4 15.3, 2 18.9).
 template <int NP>
 void launch_parts(const LinearArgs& a, hipStream_t s) {
   const int strips = a.N / 16;
-  if (a.M * NP <= 16 && static_cast<size_t>(a.M) * NP * a.K * 2 <= kStageBytes) {
-    if (strips <= 256)
-      launch_staged<NP, 1>(a, s);
-    else
-      launch_staged<NP, 2>(a, s);
+  if (staged<NP>(a)) {
+    if constexpr (NP > 1) {
+      if (strips <= 256)
+        launch_staged<NP, 1>(a, s);
+      else
+        launch_staged<NP, 2>(a, s);
+    }
   } else if (a.M <= 16) {
     if (strips <= 256)
       launch_rows<NP, 1, 1>(a, s);
