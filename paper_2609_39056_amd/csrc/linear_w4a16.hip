@@ -195,7 +195,8 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
 // kernel (16 rows of 13824 -> 5120 without a channel scaling: 22.8 us, now 13.8).
 // A wave reads only what it copied: the loop has no barriers.  With two row
 // tiles eight waves and no block ahead do better than four with one (64 rows of
-// 5120 -> 13824: 38.4 us, 42.6), where registers leave room for them.  With a
+// 5120 -> 13824: 38.4 us, 42.6), where registers leave room for them; strips of
+// 16 channels take twelve (16 rows of 8192 -> 2048 11.7 us, eight 12.7).  With a
 // scaling and 16 rows what is left is the splitting of x~ in every workgroup, 7.5
 // vector operations a value (13824 -> 5120, fp32 out: 25 us, vector units 80 %
 // busy; 13.8 without).
@@ -208,7 +209,7 @@ struct Ring {
   static constexpr int COPIES = RT * 4 + NT + 1 + (NP > 1 ? 2 : 0);
   static constexpr bool WIDE = RT == 2 && NT == 4 && NP == 3;  // the most registers
   static constexpr int SLOTS = RT == 1 || WIDE ? 2 : 1;
-  static constexpr int WAVES = WIDE ? 4 : 8;
+  static constexpr int WAVES = WIDE ? 4 : NT == 1 ? 12 : 8;
   static_assert(WAVES * SLOTS * SLOT <= 160 * 1024, "the rings fit in the LDS");
   static_assert(NT * RT * 1024 <= SLOTS * SLOT, "the waves' sums fit in the rings");
 };
