@@ -183,6 +183,8 @@ def _load_call():
         loader.exec_module(mod)
         if mod.built_for != _build.built_for():
             raise ImportError(f"built for {mod.built_for}, this is {_build.built_for()}")
+        if not hasattr(mod, "setup_token"):
+            raise ImportError("built from an older source")
     except ImportError as e:
         warnings.warn(f"{CALL_PATH}: {e}; arguments are marshalled with ctypes "
                       "(rebuild: python -m paper_2609_39056_amd._build)", RuntimeWarning, stacklevel=3)
