@@ -490,10 +490,12 @@ typedef struct sq_kv_cache {
  *   token_start          int32 [num_requests + 1] out: start of every request
  *                        and the sum of new (values past 2^31 - 1 read 2^31 - 1)
  *   kv_len               int32 [num_requests] out
- *   free_head_out        int32 [1] out; may be free_head
- * kv_len may be cached_len; otherwise outputs must not overlap inputs or each
- * other.  page_size as in sq_kv_cache, 1 <= max_pages, max_pages * page_size <
- * 2^31, num_requests * max_pages < 2^31. */
+ *   free_head_out        int32 [1] out
+ * Outputs must not overlap inputs or each other (every workgroup reads the
+ * lengths and the head): kv_len being cached_len or new_len, or free_head_out
+ * being free_head, is SQ_ERR_UNSUPPORTED.  page_size as in sq_kv_cache,
+ * 1 <= max_pages, max_pages * page_size < 2^31, num_requests * max_pages <
+ * 2^31. */
 sq_status sq_kv_plan(const int32_t* cached_len, const int32_t* new_len, int32_t num_requests, int32_t page_size,
                      const int32_t* free_pages, int32_t num_free, const int32_t* free_head, int32_t* table,
                      int32_t max_pages, int32_t max_tokens, int32_t* slot, int32_t* pos, int32_t* token_start,
