@@ -341,7 +341,7 @@ void launch_parts(const LinearArgs& a, hipStream_t s) {
       else
         launch_staged<NP, 2>(a, s);
     }
-  } else if (a.M <= 16) {
+  } else if (a.M <= 16 || strips * ((a.M + 15) / 16) <= 256) {
     if (strips <= 256)
       launch_rows<NP, 1, 1>(a, s);
     else if (strips <= 512)
