@@ -328,9 +328,15 @@ bool staged(const LinearArgs& a) {
   return NP > 1 && a.M * NP <= 6 && bytes <= (a.N / 16 <= 512 ? 144 << 10 : 80 << 10);
 }
 
-// Strips of 16 NT output channels: NT = 1 until the strips outnumber the CUs,
-// then wider ones, which share a workgroup's splitting of x~ (16 rows of
-// 13824 -> 5120, fp32 out: NT = 2 25 us, 1 40; 5120 -> 15360: NT = 4 15.3, 2 18.9).
+// The rows kernel's tiles: strips of 16 NT channels by 16 RT rows.  Narrow ones
+// make more workgroups, of which a CU has one at a time; wide ones share the
+// splitting of x~ (by channels) and the widening of codes (by rows).  A workgroup
+// takes about 4 + RT (3 NP - 1 + NT) + NT (measured with CUs to spare, 8192 channels
+// in, scaled: NT, RT = 1, 1 9.1 us, 2, 1 11.5, 4, 1 15, 4, 2 24.8 beside 3 of launch;
+// unscaled 5.6, 7, 9.7, 13.8), the call that many rounds over the CUs: 64 rows of
+// 5120 -> 5120, scaled, 4, 2 20.5 us, 4, 1 23.7, 2, 1 25.7, 1, 1 32.8; 64 of
+// 8192 -> 2048 27.9, 18.1, 14.9, 21.0; 24 of 5120 -> 5120 fp32 out 26.8, 16.4, 21.8,
+// 26.1.  Strips of 16 or 32 by 32 rows are never the best of these.
 template <int NP>
 void launch_parts(const LinearArgs& a, hipStream_t s) {
   const int strips = a.N / 16;
@@ -341,21 +347,23 @@ void launch_parts(const LinearArgs& a, hipStream_t s) {
       else
         launch_staged<NP, 2>(a, s);
     }
-  } else if (a.M <= 16 || strips * ((a.M + 15) / 16) <= 256) {
-    if (strips <= 256)
-      launch_rows<NP, 1, 1>(a, s);
-    else if (strips <= 512)
-      launch_rows<NP, 2, 1>(a, s);
-    else
-      launch_rows<NP, 4, 1>(a, s);
-  } else {
-    if (strips <= 256)
-      launch_rows<NP, 1, 2>(a, s);
-    else if (strips <= 512)
-      launch_rows<NP, 2, 2>(a, s);
-    else
-      launch_rows<NP, 4, 2>(a, s);
+    return;
   }
+  const int cus = device_cus();
+  auto cost = [&](int nt, int rt) {
+    const int wgs = strips / nt * ((a.M + 16 * rt - 1) / (16 * rt));
+    return (wgs + cus - 1) / cus * (4 + rt * (3 * NP - 1 + nt) + nt);
+  };
+  const int c11 = cost(1, 1), c21 = cost(2, 1), c41 = cost(4, 1), c42 = cost(4, 2);
+  const int least = std::min(std::min(c11, c21), std::min(c41, c42));
+  if (c11 == least)
+    launch_rows<NP, 1, 1>(a, s);
+  else if (c21 == least)
+    launch_rows<NP, 2, 1>(a, s);
+  else if (c41 == least)
+    launch_rows<NP, 4, 1>(a, s);
+  else
+    launch_rows<NP, 4, 2>(a, s);
 }
 
 }  // namespace
