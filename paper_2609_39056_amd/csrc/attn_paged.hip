@@ -126,7 +126,8 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
 
-  // blockIdx.x: key-value head, tile of query heads, split; blockIdx.y: request
+  // blockIdx.x: key-value head, tile of query heads, split (past the last one in a
+  // workgroup that only fills the row); blockIdx.y: request
   const int r = blockIdx.y;
   uint32_t wg = blockIdx.x;
   const int kvh = static_cast<int>(wg % static_cast<uint32_t>(a.Hk));
@@ -421,10 +422,23 @@ __global__ __launch_bounds__(THREADS) void attn_join_kernel(AttnArgs a, AttnSpli
   finish_row(a, row, d4, M, L, v);
 }
 
+// Workgroups of a request.  They go to the XCDs in turn, and in an XCD to its
+// shader engines, so a request's row of a multiple of 8 (or of 32) of them
+// would put split s of every request in the same place, and the last splits are
+// empty for all but the longest histories.  Split rows are therefore made odd,
+// with workgroups that find nothing and end: the splits where the heads go
+// evenly over the XCDs (128 histories up to 2048, 8 heads: 90 us, 130 in four
+// splits without), the row itself elsewhere (64 up to 8192, one head: 36 us, 47).
+unsigned grid_row(int heads, int splits) {
+  const unsigned h = static_cast<unsigned>(heads), s = static_cast<unsigned>(splits);
+  if (s == 1) return h;
+  return h % 8 == 0 ? h * (s | 1u) : (h * s) | 1u;
+}
+
 template <bool F16, int NP, int W>
 void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
   const int qt = (a.Hq / a.Hk + kQTile - 1) / kQTile;
-  const dim3 grid(static_cast<unsigned>(a.Hk * qt * sp.count), static_cast<unsigned>(a.R));
+  const dim3 grid(grid_row(a.Hk * qt, sp.count), static_cast<unsigned>(a.R));
   switch (a.D) {
     case 64: attn_kernel<F16, 64, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
     case 96: attn_kernel<F16, 96, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
@@ -455,7 +469,7 @@ hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
   const int64_t span = attn_span(a.max_kv_len, a.window);
   const AttnSplit sp = attn_split(heads, span);
   if (attn_part_bytes(a.R, a.Hq, a.D, sp.count) > a.part_bytes) return hipErrorInvalidValue;
-  if (heads / a.R * sp.count >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
+  if (heads / a.R * (sp.count + 1) >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
   if (attn_lone(heads, span))
     launch_waves<1>(a, sp, f16, s);
   else
