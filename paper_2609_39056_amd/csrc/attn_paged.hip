@@ -23,7 +23,7 @@
 // l is fp32 over the unrounded p.
 //
 // Reading the keys and values goes at 5.2 to 5.9 TB/s where there is enough of
-// it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 170 us; two histories of
+// it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 165 us; two histories of
 // 131072: 117 to 130 us; a copy of 4 GiB runs at 4.8 TB/s).  Nontemporal loads
 // are 2 to 13 % faster than cached ones, the most on long histories.  A call with
 // little to read is bound by its chain of loads (length, table entry, keys) and

@@ -3,14 +3,15 @@
 // A workgroup costs about 5 us from its launch to its last store (three
 // dependent loads, the join of its waves) and 1.2 us per 128 tokens; a split
 // adds a second kernel, 3 to 6 us.  So short spans stay whole: up to 384
-// tokens, up to 640 from 192 (request, head) pairs on (192 with 531 tokens: 22 us
-// whole, 26 in parts), and up to 1280 where the pairs alone fill the CUs (768
-// with 1055 tokens: 38 us whole, 42 in five parts, 47 in two; 1024 with up to
-// 1000: 55 whole, 68 in two).  Longer ones aim at 2048 workgroups in
-// all, eight per CU, so that ragged batches even out: 512 heads with 1024 to
-// 8192 tokens take 176 us in chunks of 512, 193 in 1024, 212 in 1152.  Spans
-// past 65536 may take chunks of 1024 (two histories of 131072, 8 heads: 136 us,
-// 142 in chunks of 512: half the parts to join).
+// tokens, up to 640 from 192 (request, head) pairs on (200 with up to 600, 32
+// query heads: 22.5 us whole, 25 in parts), and up to 1280 where the pairs alone
+// fill the CUs (768 with 1055 tokens: 37 us whole, 42 in parts; 512 with up to 700:
+// 25 and 26; 2000 with up to 1200: 104 and 106; but 1024 with up to 1000: 56 and 52).
+// Longer ones aim at 2048 workgroups in all, eight per CU, so that ragged batches
+// even out: 512 heads with 1024 to 8192 tokens take 171 us in chunks of 512, 178 in
+// 384, 169 in 640 or 768, but 512 with up to 4096 93, 95, 95 and 97.  Spans past
+// 65536 may take chunks of 1024 (two histories of 131072, 8 heads: 136 us, 142 in
+// chunks of 512: half the parts to join).
 #pragma once
 
 #include <stdint.h>
