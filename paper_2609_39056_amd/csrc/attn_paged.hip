@@ -5,7 +5,7 @@
 // bytes and query head of a group leave the matrix cores mostly idle.
 //
 // A wave takes 32 tokens at a time for up to 16 query heads of one key-value
-// head, with 16 x 16 x 32 matrix-core tiles and nothing passed between lanes:
+// head (or two such tiles), with 16 x 16 x 32 matrix-core tiles and nothing passed between lanes:
 //   scores   A = 16 keys (lane: key lane & 15, values 32 j + 8 (lane >> 4) ..),
 //            B = the queries; lane (c, g) gets head c, tokens 4 g .. 4 g + 3 of
 //            each half of the tile
@@ -28,6 +28,8 @@
 // are 2 to 13 % faster than cached ones, the most on long histories.  A call with
 // little to read is bound by its chain of loads (length, table entry, keys) and
 // one launch: 5 to 7 us.
+#include <type_traits>
+
 #include "attn_split.h"
 #include "half_types.h"
 #include "token_internal.h"
@@ -104,8 +106,8 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, size_t row, int d4
   if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
 }
 
-// W waves take a chunk.
-template <bool F16, int D, int NP, int W>
+// W waves take a chunk, for Q tiles of 16 query heads.
+template <bool F16, int D, int NP, int W, int Q>
 __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
   constexpr int KF = D / 32;  // fragments of a key row
   // a lane's part of a value row: E dimensions, E0 c .. of the first 16 E0 and
@@ -121,7 +123,8 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
   constexpr float kShift = F16 ? 11.0f : 0.0f;
   constexpr float kSlack = F16 ? 4.0f : 8.0f;
   __shared__ int32_t pages[kPages];
-  __shared__ float s_m[W][kQTile], s_l[W][kQTile], s_o[W][kQTile][D + 4];
+  constexpr int kHeads = Q * kQTile;
+  __shared__ float s_m[W][kHeads], s_l[W][kHeads], s_o[W][kHeads][D + 4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -135,8 +138,8 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
   const int qt = static_cast<int>(wg % static_cast<uint32_t>(qtiles));
   const int split = static_cast<int>(wg / static_cast<uint32_t>(qtiles));
   const int G = a.Hq / a.Hk;
-  const int gq = min(G - qt * kQTile, kQTile);  // query heads here
-  const int h0 = kvh * G + qt * kQTile;
+  const int gq = min(G - qt * kHeads, kHeads);  // query heads here
+  const int h0 = kvh * G + qt * kHeads;
 
   // Without a window the chunk's table entries do not wait for the length
   // (those past it are in the row all the same, and not used).
@@ -157,20 +160,29 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
   const int page0 = begin >> shift;
   const int npages = begin < end ? ((end - 1) >> shift) - page0 + 1 : 0;
 
-  // queries: column c is head h0 + c, the lane's values 32 j + 8 g ..
-  uint4 q[KF];
-  const uint16_t* qrow = a.q + r * a.q_stride + static_cast<size_t>(h0 + min(c, gq - 1)) * D + 8 * g;
+  // queries: column c of tile y is head h0 + 16 y + c, the lane's values 32 j + 8 g ..
+  uint4 q[Q][KF];
 #pragma unroll
-  for (int j = 0; j < KF; ++j) {
-    q[j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
-    if (c >= gq) q[j] = make_uint4(0, 0, 0, 0);
+  for (int y = 0; y < Q; ++y) {
+    const int h = kQTile * y + c;
+    const uint16_t* qrow = a.q + r * a.q_stride + static_cast<size_t>(h0 + min(h, gq - 1)) * D + 8 * g;
+#pragma unroll
+    for (int j = 0; j < KF; ++j) {
+      q[y][j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
+      if (h >= gq) q[y][j] = make_uint4(0, 0, 0, 0);
+    }
   }
   __syncthreads();
 
-  v4f o[E];
+  v4f o[Q][E];
+  float m[Q], l[Q];
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = v4f{0, 0, 0, 0};
-  float m = kLowest, l = 0.0f;
+  for (int y = 0; y < Q; ++y) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[y][e] = v4f{0, 0, 0, 0};
+    m[y] = kLowest;
+    l[y] = 0.0f;
+  }
   const float scale = a.scale * kLog2e;
 
   auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
@@ -225,16 +237,18 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
       load_k(b);
       load_v(b);
     }
-    v4f s[2];
+    float f[Q][8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      s[i] = v4f{0, 0, 0, 0};
+    for (int y = 0; y < Q; ++y) {
 #pragma unroll
-      for (int j = 0; j < KF; ++j) s[i] = mfma<F16>(k[i][j], q[j], s[i]);
+      for (int i = 0; i < 2; ++i) {
+        v4f s = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < KF; ++j) s = mfma<F16>(k[i][j], q[y][j], s);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[x] * scale;
+      }
     }
-    float f[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = s[i / 4][i % 4] * scale;
     const bool whole_tile = inside(b) && __all(kp[0] >= 0 && kp[1] >= 0);
     if (kAhead && t + W < tiles) load_k(b + W * kTile);
     if (!whole_tile) {
@@ -242,33 +256,37 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
       for (int i = 0; i < 8; ++i) {
         const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
         const bool live = (tok >= first) & (tok < end) & (vp[i / 4] >= 0);
-        f[i] = live ? f[i] : -INFINITY;
+#pragma unroll
+        for (int y = 0; y < Q; ++y) f[y][i] = live ? f[y][i] : -INFINITY;
 #pragma unroll
         for (int w = 0; w < EW; ++w) v[i][w] = live ? v[i][w] : 0;
       }
     }
-    float top = f[0];
+    uint32_t p[Q][NP][4];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, f[i]);
-    if (__any(top > m + kSlack)) {
-      const float mn = fmaxf(m, quad_max(top));
-      const float al = __builtin_amdgcn_exp2f(m - mn);
-      m = mn;
-      l *= al;
+    for (int y = 0; y < Q; ++y) {
+      float top = f[y][0];
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= al;
-    }
-    uint32_t p[NP][4];
-    const float base = m - kShift;
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, f[y][i]);
+      if (__any(top > m[y] + kSlack)) {
+        const float mn = fmaxf(m[y], quad_max(top));
+        const float al = __builtin_amdgcn_exp2f(m[y] - mn);
+        m[y] = mn;
+        l[y] *= al;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float x = __builtin_amdgcn_exp2f(f[i] - base), y = __builtin_amdgcn_exp2f(f[i + 1] - base);
-      l += x + y;
+        for (int e = 0; e < E; ++e) o[y][e] *= al;
+      }
+      const float base = m[y] - kShift;
 #pragma unroll
-      for (int u = 0; u < NP; ++u) {
-        p[u][i / 2] = to_half2<F16>(x, y);
-        x -= half_lo<F16>(p[u][i / 2]);
-        y -= half_hi<F16>(p[u][i / 2]);
+      for (int i = 0; i < 8; i += 2) {
+        float x0 = __builtin_amdgcn_exp2f(f[y][i] - base), x1 = __builtin_amdgcn_exp2f(f[y][i + 1] - base);
+        l[y] += x0 + x1;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          p[y][u][i / 2] = to_half2<F16>(x0, x1);
+          x0 -= half_lo<F16>(p[y][u][i / 2]);
+          x1 -= half_hi<F16>(p[y][u][i / 2]);
+        }
       }
     }
 #pragma unroll
@@ -280,22 +298,29 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
       vt.z = __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel);
       vt.w = __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel);
 #pragma unroll
-      for (int u = 0; u < NP; ++u) o[e] = mfma<F16>(vt, make_uint4(p[u][0], p[u][1], p[u][2], p[u][3]), o[e]);
+      for (int y = 0; y < Q; ++y)
+#pragma unroll
+        for (int u = 0; u < NP; ++u)
+          o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
     }
     if (kAhead && t + W < tiles) load_v(b + W * kTile);
   }
 
   // the waves' parts: column c, and the dimensions that lane 4 g + x loaded
-  l = quad_sum(l);
-  if (g == 0) {
-    s_m[wave][c] = m - kShift;
-    s_l[wave][c] = l;
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+    const int h = kQTile * y + c;
+    const float ls = quad_sum(l[y]);
+    if (g == 0) {
+      s_m[wave][h] = m[y] - kShift;
+      s_l[wave][h] = ls;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (h < gq) s_o[wave][h][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[y][e][x];
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (c < gq) s_o[wave][c][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[e][x];
   __syncthreads();
   for (int i = threadIdx.x; i < gq * (D / 4); i += 64 * W) {
     const int qh = i / (D / 4), d4 = i % (D / 4);
@@ -435,16 +460,37 @@ unsigned grid_row(int heads, int splits) {
   return h % 8 == 0 ? h * (s | 1u) : (h * s) | 1u;
 }
 
+// More than 16 query heads on a key-value head (head dimensions up to 128, whose
+// registers leave room): where one tile each would make as many workgroups as
+// CUs, for spans past 384, a workgroup takes two and reads the keys and values
+// once for them (32 heads on one, 64 histories up to 8192: 45 us, 62 in workgroups
+// of a tile; 200 up to 600: 18.1, 22.6; 10 up to 2000: 12.8, 13.1; but 4 up to 2000
+// 12.1 and 10.9, 130 up to 300 9.7 and 9.3).
+template <bool F16, int NP, int W, int D>
+void launch_tiles(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
+  const int G = a.Hq / a.Hk;
+  auto launch = [&](auto tiles) {
+    constexpr int Q = decltype(tiles)::value;
+    const int qt = (G + Q * kQTile - 1) / (Q * kQTile);
+    const dim3 grid(grid_row(a.Hk * qt, sp.count), static_cast<unsigned>(a.R));
+    attn_kernel<F16, D, NP, W, Q><<<grid, 64 * W, 0, s>>>(a, sp, qt);
+  };
+  if constexpr (D <= 128 && W > 1) {
+    if (G > kQTile && attn_span(a.max_kv_len, a.window) > 384 &&
+        attn_heads(a.R, a.Hq, a.Hk) * sp.count >= device_cus())
+      return launch(std::integral_constant<int, 2>{});
+  }
+  launch(std::integral_constant<int, 1>{});
+}
+
 template <bool F16, int NP, int W>
 void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
-  const int qt = (a.Hq / a.Hk + kQTile - 1) / kQTile;
-  const dim3 grid(grid_row(a.Hk * qt, sp.count), static_cast<unsigned>(a.R));
   switch (a.D) {
-    case 64: attn_kernel<F16, 64, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
-    case 96: attn_kernel<F16, 96, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
-    case 128: attn_kernel<F16, 128, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
-    case 192: attn_kernel<F16, 192, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
-    default: attn_kernel<F16, 256, NP, W><<<grid, 64 * W, 0, s>>>(a, sp, qt); break;
+    case 64: return launch_tiles<F16, NP, W, 64>(a, sp, s);
+    case 96: return launch_tiles<F16, NP, W, 96>(a, sp, s);
+    case 128: return launch_tiles<F16, NP, W, 128>(a, sp, s);
+    case 192: return launch_tiles<F16, NP, W, 192>(a, sp, s);
+    default: return launch_tiles<F16, NP, W, 256>(a, sp, s);
   }
 }
 

@@ -268,6 +268,18 @@ def test_attn_heads(Hq, Hk, D, dtype):
         check_attn(attn_case(4, L, Hq, Hk, D, page, dtype, Hq + D + L), out)
 
 
+@pytest.mark.parametrize("Hq,Hk,D,page,dtype,out", [
+    (32, 1, 128, 16, "bf16", "f32"), (17, 1, 64, 8, "f16", "f16"), (40, 1, 96, 64, "bf16", "bf16"),
+    (72, 2, 128, 32, "f16", "f32")])
+def test_attn_many_heads_of_one(Hq, Hk, D, page, dtype, out):
+    """Enough requests of long and short histories that a workgroup takes 32 query heads, whole and split."""
+    for R, L in ((130, 410), (12, 1700)):
+        lens = ([L, 0, 1, 33, L - 1, 300, 31, 32] + [(37 * r) % 90 for r in range(R)])[:R]
+        c = attn_case(R, L, Hq, Hk, D, page, dtype, Hq + L, lens=lens)
+        check_attn(c, out)
+        check_attn(c, out, window=390)
+
+
 def test_attn_short_lengths():
     """Every length around the tile's and the page's ends, in one batch."""
     lens = list(range(0, 70)) + [127, 128, 129, 255, 256, 257]
