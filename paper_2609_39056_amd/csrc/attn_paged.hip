@@ -475,7 +475,7 @@ void launch_tiles(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
     const dim3 grid(grid_row(a.Hk * qt, sp.count), static_cast<unsigned>(a.R));
     attn_kernel<F16, D, NP, W, Q><<<grid, 64 * W, 0, s>>>(a, sp, qt);
   };
-  if constexpr (D <= 128 && W > 1) {
+  if constexpr (D <= 128 && W == 4) {
     if (G > kQTile && attn_span(a.max_kv_len, a.window) > 384 &&
         attn_heads(a.R, a.Hq, a.Hk) * sp.count >= device_cus())
       return launch(std::integral_constant<int, 2>{});
@@ -516,8 +516,13 @@ hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
   const AttnSplit sp = attn_split(heads, span);
   if (attn_part_bytes(a.R, a.Hq, a.D, sp.count) > a.part_bytes) return hipErrorInvalidValue;
   if (heads / a.R * (sp.count + 1) >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
+  // A whole span is a chain of tiles: eight waves shorten it where a workgroup has
+  // a CU to itself (30 requests of up to 350 tokens, 8 heads of 64: 8.0 us, four
+  // waves 8.9; 28 of 600 with heads of 128 14.1, 15.7; with 512 heads of 500 20.3, 19.5).
   if (attn_lone(heads, span))
     launch_waves<1>(a, sp, f16, s);
+  else if (sp.count == 1 && span > 128 && heads <= device_cus())
+    launch_waves<8>(a, sp, f16, s);
   else
     launch_waves<4>(a, sp, f16, s);
   hipError_t e = hipGetLastError();
