@@ -193,30 +193,31 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
 // bytes (16 of 64) per instruction; loads in the fragments' own layout touch a
 // line with every lane, and those kept the address unit busy for the whole
 // kernel (16 rows of 13824 -> 5120 without a channel scaling: 22.8 us, now 13.8).
-// A wave reads only what it copied: the loop has no barriers.  With two row
-// tiles eight waves and no block ahead do better than four with one (64 rows of
-// 5120 -> 13824: 38.4 us, 42.6), where registers leave room for them; strips of
-// 16 channels take twelve (16 rows of 8192 -> 2048 11.7 us, eight 12.7).  With a
+// A wave reads only what it copied: the loop has no barriers.  W waves: eight,
+// twelve for strips of 16 channels (16 rows of 8192 -> 2048 11.7 us, eight 12.7).
+// With two row tiles there is no block ahead (64 rows of 5120 -> 13824, scaled: 38.4
+// us, 42.6 in four waves with one), and where workgroups outnumber the CUs they are
+// of four waves, two to a CU (36.0; unscaled 22.5, eight waves 25.6; but 64 rows of
+// 5120 -> 5120, unscaled, with CUs to spare 17.0 and 13.5).  With a
 // scaling and 16 rows what is left is the splitting of x~ in every workgroup, 7.5
 // vector operations a value (13824 -> 5120, fp32 out: 25 us, vector units 80 %
 // busy; 13.8 without).
-template <int NP, int NT, int RT>
+template <int NP, int NT, int RT, int NW>
 struct Ring {
   static constexpr int X = RT * 16 * 2 * kBlock;    // row r, 16-byte chunk k at r * 256 + 16 * (k ^ (r & 15))
   static constexpr int W = NT * 16 * (kBlock / 2);  // channel n, chunk k at n * 64 + 16 * (k ^ ((n >> 2) & 3))
   static constexpr int W_OFF = X, S_OFF = X + W, D_OFF = S_OFF + 256;
   static constexpr int SLOT = D_OFF + (NP > 1 ? 4 * kBlock : 0);
   static constexpr int COPIES = RT * 4 + NT + 1 + (NP > 1 ? 2 : 0);
-  static constexpr bool WIDE = RT == 2 && NT == 4 && NP == 3;  // the most registers
-  static constexpr int SLOTS = RT == 1 || WIDE ? 2 : 1;
-  static constexpr int WAVES = WIDE ? 4 : NT == 1 ? 12 : 8;
+  static constexpr int SLOTS = RT == 1 ? 2 : 1;
+  static constexpr int WAVES = NW;
   static_assert(WAVES * SLOTS * SLOT <= 160 * 1024, "the rings fit in the LDS");
   static_assert(NT * RT * 1024 <= SLOTS * SLOT, "the waves' sums fit in the rings");
 };
 
-template <int NP, int NT, int RT>
-__global__ __launch_bounds__((64 * Ring<NP, NT, RT>::WAVES)) void linear_rows_kernel(LinearArgs a) {
-  using L = Ring<NP, NT, RT>;
+template <int NP, int NT, int RT, int W>
+__global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void linear_rows_kernel(LinearArgs a) {
+  using L = Ring<NP, NT, RT, W>;
   __shared__ __attribute__((aligned(16))) uint8_t ring[L::WAVES][L::SLOTS][L::SLOT];
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -312,10 +313,10 @@ void launch_staged(const LinearArgs& a, hipStream_t s) {
   linear_staged_kernel<NP, NT><<<grid, 64 * waves, bytes, s>>>(a);
 }
 
-template <int NP, int NT, int RT>
+template <int NP, int NT, int RT, int W>
 void launch_rows(const LinearArgs& a, hipStream_t s) {
   const dim3 grid(a.N / (16 * NT), (a.M + 16 * RT - 1) / (16 * RT));
-  linear_rows_kernel<NP, NT, RT><<<grid, 64 * Ring<NP, NT, RT>::WAVES, 0, s>>>(a);
+  linear_rows_kernel<NP, NT, RT, W><<<grid, 64 * W, 0, s>>>(a);
 }
 
 // Whether the staged kernel takes the layer: up to six rows of parts (two rows
@@ -357,13 +358,15 @@ void launch_parts(const LinearArgs& a, hipStream_t s) {
   const int c11 = cost(1, 1), c21 = cost(2, 1), c41 = cost(4, 1), c42 = cost(4, 2);
   const int least = std::min(std::min(c11, c21), std::min(c41, c42));
   if (c11 == least)
-    launch_rows<NP, 1, 1>(a, s);
+    launch_rows<NP, 1, 1, 12>(a, s);
   else if (c21 == least)
-    launch_rows<NP, 2, 1>(a, s);
+    launch_rows<NP, 2, 1, 8>(a, s);
   else if (c41 == least)
-    launch_rows<NP, 4, 1>(a, s);
+    launch_rows<NP, 4, 1, 8>(a, s);
+  else if (strips / 4 * ((a.M + 31) / 32) <= cus)
+    launch_rows<NP, 4, 2, 8>(a, s);
   else
-    launch_rows<NP, 4, 2>(a, s);
+    launch_rows<NP, 4, 2, 4>(a, s);
 }
 
 }  // namespace

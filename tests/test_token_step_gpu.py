@@ -425,6 +425,21 @@ def test_linear(M, K, N, group, out):
         T.check(y[:M], want, bound, DT[out], "y")
 
 
+@pytest.mark.parametrize("M,K,N,group", [(13, 1152, 5120, 128), (30, 1408, 2112, 128), (29, 384, 4736, 384),
+                                         (47, 1152, 5120, 1152), (64, 128, 6144, 128), (37, 1152, 8256, 128),
+                                         (64, 640, 9024, 640), (33, 128, 13824, 128)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_linear_tiles(M, K, N, group, out):
+    """Wide strips and two row tiles, with CUs to spare and without, ragged rows and blocks."""
+    for use_d in (True, False):
+        x, dinv, W, bias = linear_case(M, K, N, group, use_d, True, M + K + N)
+        y = torch.full((M + 1, N), float("nan"), dtype=DT[out], device="cuda")
+        B.sq_linear_w4a16(x.cuda(), dev(dinv), W, y[:M], OUT[out])
+        assert torch.isnan(y[M]).all()
+        want, bound = T.linear(x, dinv, W.qw.cpu().numpy(), W.w_scale.cpu(), group, bias, DT[out])
+        T.check(y[:M], want, bound, DT[out], "y")
+
+
 def test_linear_all_codes():
     """Every nibble, -8 included (the packer writes -7 .. 7, the product takes
     what a nibble holds), on integers: exact."""
