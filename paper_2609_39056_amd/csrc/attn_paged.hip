@@ -16,11 +16,11 @@
 //            sums come as lane (c, g): head c, dimensions of lanes 4 g ..
 // The maximum is only moved when some score exceeds it by 8 (bf16: p up to
 // 2^8) or 4 (f16, whose p are scaled by 2^11 to keep small ones off its
-// subnormals), which leaves out most rescaling.  p enters its product as 16-bit
-// parts, the second (and for fp32 outputs third bf16) part holding what the
-// first left, so that outputs carry only their own rounding (bf16 p alone would
-// add about as much again); the products are hidden behind the loads.  The sum
-// l is fp32 over the unrounded p.
+// subnormals), which leaves out most rescaling.  p enters its product as three
+// 16-bit parts, each holding what the ones before left: all 24 bits of it, whatever
+// the output's type.  The products are hidden behind the loads (64 requests up to
+// 8192 tokens, 8 heads of 128: 171 us, two parts 170; 100 of 64 tokens, 40 heads
+// 18.2 and 18.0).  The sum l is fp32 over the unrounded p.
 //
 // Reading the keys and values goes at 5.2 to 5.9 TB/s where there is enough of
 // it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 165 us; two histories of
@@ -39,6 +39,7 @@ namespace {
 
 constexpr int kTile = kAttnTile, kQTile = kAttnQTile;  // kQTile: the columns of a 16 x 16 matrix-core tile
 constexpr int kMinPage = 8;
+constexpr int kParts = 3;  // 16-bit parts of a probability
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;  // no score yet
@@ -107,7 +108,7 @@ __device__ __forceinline__ void finish_row(const AttnArgs& a, size_t row, int d4
 }
 
 // W waves take a chunk, for Q tiles of 16 query heads.
-template <bool F16, int D, int NP, int W, int Q>
+template <bool F16, int D, int W, int Q>
 __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs a, AttnSplit sp, int qtiles) {
   constexpr int KF = D / 32;  // fragments of a key row
   // a lane's part of a value row: E dimensions, E0 c .. of the first 16 E0 and
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
         for (int w = 0; w < EW; ++w) v[i][w] = live ? v[i][w] : 0;
       }
     }
-    uint32_t p[Q][NP][4];
+    uint32_t p[Q][kParts][4];
 #pragma unroll
     for (int y = 0; y < Q; ++y) {
       float top = f[y][0];
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
         float x0 = __builtin_amdgcn_exp2f(f[y][i] - base), x1 = __builtin_amdgcn_exp2f(f[y][i + 1] - base);
         l[y] += x0 + x1;
 #pragma unroll
-        for (int u = 0; u < NP; ++u) {
+        for (int u = 0; u < kParts; ++u) {
           p[y][u][i / 2] = to_half2<F16>(x0, x1);
           x0 -= half_lo<F16>(p[y][u][i / 2]);
           x1 -= half_hi<F16>(p[y][u][i / 2]);
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
 #pragma unroll
       for (int y = 0; y < Q; ++y)
 #pragma unroll
-        for (int u = 0; u < NP; ++u)
+        for (int u = 0; u < kParts; ++u)
           o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
     }
     if (kAhead && t + W < tiles) load_v(b + W * kTile);
@@ -466,14 +467,14 @@ unsigned grid_row(int heads, int splits) {
 // once for them (32 heads on one, 64 histories up to 8192: 45 us, 62 in workgroups
 // of a tile; 200 up to 600: 18.1, 22.6; 10 up to 2000: 12.8, 13.1; but 4 up to 2000
 // 12.1 and 10.9, 130 up to 300 9.7 and 9.3).
-template <bool F16, int NP, int W, int D>
+template <bool F16, int W, int D>
 void launch_tiles(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
   const int G = a.Hq / a.Hk;
   auto launch = [&](auto tiles) {
     constexpr int Q = decltype(tiles)::value;
     const int qt = (G + Q * kQTile - 1) / (Q * kQTile);
     const dim3 grid(grid_row(a.Hk * qt, sp.count), static_cast<unsigned>(a.R));
-    attn_kernel<F16, D, NP, W, Q><<<grid, 64 * W, 0, s>>>(a, sp, qt);
+    attn_kernel<F16, D, W, Q><<<grid, 64 * W, 0, s>>>(a, sp, qt);
   };
   if constexpr (D <= 128 && W == 4) {
     if (G > kQTile && attn_span(a.max_kv_len, a.window) > 384 &&
@@ -483,25 +484,15 @@ void launch_tiles(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
   launch(std::integral_constant<int, 1>{});
 }
 
-template <bool F16, int NP, int W>
+template <bool F16, int W>
 void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
   switch (a.D) {
-    case 64: return launch_tiles<F16, NP, W, 64>(a, sp, s);
-    case 96: return launch_tiles<F16, NP, W, 96>(a, sp, s);
-    case 128: return launch_tiles<F16, NP, W, 128>(a, sp, s);
-    case 192: return launch_tiles<F16, NP, W, 192>(a, sp, s);
-    default: return launch_tiles<F16, NP, W, 256>(a, sp, s);
+    case 64: return launch_tiles<F16, W, 64>(a, sp, s);
+    case 96: return launch_tiles<F16, W, 96>(a, sp, s);
+    case 128: return launch_tiles<F16, W, 128>(a, sp, s);
+    case 192: return launch_tiles<F16, W, 192>(a, sp, s);
+    default: return launch_tiles<F16, W, 256>(a, sp, s);
   }
-}
-
-template <int W>
-void launch_waves(const AttnArgs& a, const AttnSplit& sp, bool f16, hipStream_t s) {
-  if (f16)
-    launch_dim<true, 2, W>(a, sp, s);
-  else if (a.out_dtype == SQ_OUT_F32)
-    launch_dim<false, 3, W>(a, sp, s);
-  else
-    launch_dim<false, 2, W>(a, sp, s);
 }
 
 }  // namespace
@@ -520,11 +511,11 @@ hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {
   // a CU to itself (30 requests of up to 350 tokens, 8 heads of 64: 8.0 us, four
   // waves 8.9; 28 of 600 with heads of 128 14.1, 15.7; with 512 heads of 500 20.3, 19.5).
   if (attn_lone(heads, span))
-    launch_waves<1>(a, sp, f16, s);
+    f16 ? launch_dim<true, 1>(a, sp, s) : launch_dim<false, 1>(a, sp, s);
   else if (sp.count == 1 && span > 128 && heads <= device_cus())
-    launch_waves<8>(a, sp, f16, s);
+    f16 ? launch_dim<true, 8>(a, sp, s) : launch_dim<false, 8>(a, sp, s);
   else
-    launch_waves<4>(a, sp, f16, s);
+    f16 ? launch_dim<true, 4>(a, sp, s) : launch_dim<false, 4>(a, sp, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.count == 1) return e;
   const dim3 rows = wg_grid(static_cast<size_t>(a.R) * a.Hq * (a.D / 32));

@@ -1,0 +1,106 @@
+"""The token step's operators on the GPU with inputs whose exact result is known
+to more than a general bound can tell: sums that cancel, values that mark every
+token, infinities and NaN where they are read."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_39056_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+OUT = {"bf16": B.SQ_OUT_BF16, "f16": B.SQ_OUT_F16, "f32": B.SQ_OUT_F32}
+U = 2.0 ** -24  # the fp32 unit
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def attend(q, k, v, lens, page, out, window=0, scale=1.0, longest=None):
+    """q [R, Hq, D]; k, v [R, L, Hk, D] on the host, put into pages in a shuffled
+    order; the tokens past a request's length hold NaN.  Returns out and lse."""
+    R, L, Hk, D = k.shape
+    n = -(-L // page)
+    ids = torch.randperm(R * n, generator=torch.Generator().manual_seed(R + L)).view(R, n)
+    cache = []
+    for t in (k, v):
+        pages = torch.full((R, n * page, Hk, D), float("nan"), dtype=t.dtype)
+        for r, m in enumerate(lens):
+            pages[r, :m] = t[r, :m]
+        c = torch.empty((R * n, Hk, page, D), dtype=t.dtype)
+        c[ids.flatten()] = pages.view(R * n, page, Hk, D).transpose(1, 2)
+        cache.append(c.cuda())
+    kv = B.KVCache(*cache)
+    Hq = q.shape[1]
+    longest = L if longest is None else longest
+    y = torch.full((R, Hq, D), 77.0, dtype=DT[out], device="cuda")
+    lse = torch.full((R, Hq), 77.0, device="cuda")
+    ws = B.alloc_attn_workspace(R, Hq, kv, longest)
+    ws.fill_(255)  # NaN patterns
+    B.sq_attn_paged(q.cuda(), kv, ids.to(torch.int32).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                    longest, window, scale, y, OUT[out], lse, ws)
+    return y.cpu(), lse.cpu()
+
+
+# ------------------------------------------------------------------ probabilities
+def halves(x, dtype, parts):
+    """x (float32 numpy) as the sum of this many values of a 16-bit type, each
+    taking what the ones before left, and what they leave."""
+    rest, total = x.astype(np.float32), np.zeros(x.shape)
+    for _ in range(parts):
+        p = torch.from_numpy(rest).to(dtype).float().numpy()
+        total += p
+        rest = rest - p
+    return total, x - total
+
+
+def cancelling(D, dtype, seed):
+    """Twelve keys whose probabilities two bf16 parts hold worst (0.5 .. 0.6 of
+    the largest, with a residual of nearly 2^-18), values with the residuals'
+    signs, and four keys of probability one whose values cancel the sum."""
+    rng = np.random.default_rng(seed)
+    s = -np.arange(64, 90, dtype=np.float64) / 128  # exact in both types
+    p = np.exp(s)
+    _, rest = halves(p.astype(np.float32), torch.bfloat16, 2)
+    best = np.argsort(-np.abs(rest) / p)[:12]
+    v = np.sign(rest[best])[:, None] * torch.from_numpy(rng.uniform(0.5, 1, (12, D))).to(dtype).double().numpy()
+    scores, values = list(s[best]), list(v)
+    for _ in range(4):
+        total = sum(math.exp(a) * b for a, b in zip(scores, values))
+        scores.append(0.0)
+        values.append(-torch.from_numpy(total).to(dtype).double().numpy())
+    return np.array(scores), np.stack(values), np.abs(rest[best])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L,at", [(16, 0), (300, 96), (700, 640), (5000, 1536)])
+def test_attn_probabilities_are_whole(dtype, L, at):
+    """16-bit outputs too are sums over fp32 probabilities: a score's three
+    roundings in units of log 2 make 6 units of p (|s| < 1 and a factor of log2 e),
+    the exponential 2, the parts 1, sixteen sums of exact products up to 18 and the
+    quotient and rounding of a result that cancels to nothing none; 32 in all, of
+    the sum of magnitudes.  The other tokens' probabilities are 0."""
+    D, dt = 64, DT[dtype]
+    s, v, rest = cancelling(D, dt, L)
+    p = np.exp(s)
+    bound = 32 * U * (p[:, None] * np.abs(v)).sum(0)
+    assert ((rest[:, None] * np.abs(v[:12])).sum(0) > 1.3 * bound).all()  # what two bf16 parts would leave is outside
+    k = torch.zeros((1, L, 1, D))
+    k[0, :, 0, 0] = -200.0
+    k[0, at:at + 16, 0, 0] = torch.from_numpy(s).float()
+    vals = torch.ones((1, L, 1, D))
+    vals[0, at:at + 16, 0] = torch.from_numpy(v).float()
+    q = torch.zeros((1, 3, D))
+    q[:, :, 0] = 1.0
+    y, _ = attend(q.to(dt), k.to(dt), vals.to(dt), [L], 16, dtype)
+    want = (p[:, None] * v).sum(0) / p.sum()
+    bound = bound / p.sum()
+    err = np.abs(y[0].double().numpy() - want[None])
+    assert (err <= bound + np.abs(want) * 2.0 ** -8).all(), f"{(err / bound).max():.3g} of the bound"
