@@ -100,11 +100,13 @@ __device__ __forceinline__ void add_scaled(float4& y, const float4& v, float al)
 }
 
 // Four outputs of a query head, and its lse once, from the maximum (in units
-// of log 2), the sum and the weighted values.  An empty sum gives 0.
+// of log 2), the sum and the weighted values.  An empty sum gives 0; one that is
+// NaN (of a NaN score, or one of +infinity) goes into both.
 __device__ __forceinline__ void finish_row(const AttnArgs& a, size_t row, int d4, float M, float L, const float4& y) {
-  const float inv = L > 0.0f ? 1.0f / L : 0.0f;
+  const bool empty = L == 0.0f;
+  const float inv = empty ? 0.0f : 1.0f / L;
   store_out4(a.out, row * (a.D / 4) + d4, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv), a.out_dtype);
-  if (d4 == 0 && a.lse != nullptr) a.lse[row] = L > 0.0f ? (M + __builtin_amdgcn_logf(L)) * kLn2 : -INFINITY;
+  if (d4 == 0 && a.lse != nullptr) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
 // W waves take a chunk, for Q tiles of 16 query heads.

@@ -104,3 +104,46 @@ def test_attn_probabilities_are_whole(dtype, L, at):
     bound = bound / p.sum()
     err = np.abs(y[0].double().numpy() - want[None])
     assert (err <= bound + np.abs(want) * 2.0 ** -8).all(), f"{(err / bound).max():.3g} of the bound"
+
+
+# ------------------------------------------------------------------ values that are not finite
+def spread(R, L, Hq, Hk, D, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(s, generator=g).to(DT[dtype]) for s in ((R, Hq, D), (R, L, Hk, D), (R, L, Hk, D))]
+
+
+LENGTHS = [(24, 64), (60, 64), (300, 128), (700, 96), (2500, 64), (2500, 256)]  # one wave and more, whole and split
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L,D", LENGTHS)
+def test_attn_nan_that_is_read_is_not_an_empty_row(dtype, L, D):
+    """A NaN in an attended key or a query, or a score of +infinity, makes out and
+    lse NaN; only a row that attends nothing has lse -infinity."""
+    q, k, v = spread(5, L, 4, 2, D, dtype, L)
+    k[0, L // 2, 1, 5] = float("nan")
+    q[1, 2, 7] = float("nan")
+    k[2, L - 1, 0, 0], k[2, L - 1, 0, 1] = float("inf"), float("-inf")
+    k[4, 0, 1, 3] = float("inf")
+    q[2, :2], q[4, 2:] = 1.0, 1.0
+    y, lse = attend(q, k, v, [L, L, L, 0, L - 1], 16, dtype, scale=D ** -0.5)
+    bad = torch.zeros((5, 4), dtype=torch.bool)
+    bad[0, 2:], bad[1, 2], bad[2, :2], bad[4, 2:] = True, True, True, True
+    assert torch.equal(torch.isnan(lse), bad) and torch.equal(torch.isnan(y), bad[:, :, None].expand_as(y))
+    assert torch.isfinite(lse[[0, 1, 2, 4]][~bad[[0, 1, 2, 4]]]).all()
+    assert (lse[3] == -math.inf).all() and (y[3] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L,D", LENGTHS)
+def test_attn_scores_of_minus_infinity(dtype, L, D):
+    """An attended key whose score is -infinity has probability 0; a row of
+    nothing else is like one that attends nothing."""
+    q, k, v = spread(2, L, 2, 1, D, dtype, 2 * L + D)
+    q[:, :, 0] = 1.0
+    ref = attend(q, k[:, :L - 1], v[:, :L - 1], [L - 1, L - 1], 16, "f32", scale=D ** -0.5, longest=L)
+    k[0, L - 1, 0, 0] = float("-inf")
+    k[1, :, 0, 0] = float("-inf")
+    y, lse = attend(q, k, v, [L, L], 16, "f32", scale=D ** -0.5)
+    assert torch.equal(y[0], ref[0][0]) and torch.equal(lse[0], ref[1][0])
+    assert (y[1] == 0).all() and (lse[1] == -math.inf).all()
