@@ -550,7 +550,9 @@ size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_k
  * and lse = log sum_j exp(s_j).  Token j is row j % page_size of page
  * table[r][j / page_size]; tokens of a page number outside [0, num_pages) are
  * not attended.  Where nothing is attended, or all scores are -infinity, out
- * is 0 and lse -infinity; a score of NaN or +infinity makes both NaN.  Cache
+ * is 0 and lse -infinity; a score of NaN or +infinity makes both NaN.  An
+ * infinite value that is attended makes its output infinite (NaN beside one of
+ * the other sign, or where its probability is 0 in fp32).  Cache
  * rows that are not attended may hold anything, NaN included.  Sums, maxima
  * and probabilities' products are carried in fp32 accuracy (probabilities
  * enter the matrix cores as sums of 16-bit parts); results do not depend on

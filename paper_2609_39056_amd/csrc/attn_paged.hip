@@ -20,7 +20,9 @@
 // 16-bit parts, each holding what the ones before left: all 24 bits of it, whatever
 // the output's type.  The products are hidden behind the loads (64 requests up to
 // 8192 tokens, 8 heads of 128: 171 us, two parts 170; 100 of 64 tokens, 40 heads
-// 18.2 and 18.0).  The sum l is fp32 over the unrounded p.
+// 18.2 and 18.0).  The sum l is fp32 over the unrounded p.  Parts of p may be 0 or
+// negative, so an infinite value leaves NaN in its dimension's sum; where one is
+// NaN (and l is not) the infinities are summed by themselves at the end.
 //
 // Reading the keys and values goes at 5.2 to 5.9 TB/s where there is enough of
 // it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 165 us; two histories of
@@ -56,6 +58,8 @@ __device__ __forceinline__ v4f mfma(const uint4& x, const uint4& y, v4f c) {
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
+
+__device__ __forceinline__ bool is_nan(float v) { return v != v; }
 
 // Maximum / sum over the four lanes that share lane & 15.
 __device__ __forceinline__ float quad_max(float v) {
@@ -325,19 +329,22 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
         if (h < gq) s_o[wave][h][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[y][e][x];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < gq * (D / 4); i += 64 * W) {
-    const int qh = i / (D / 4), d4 = i % (D / 4);
-    float M = s_m[0][qh];
+  // four dimensions of a query head: maximum and sum, and the weighted values
+  auto joined = [&](int qh, int d4, float& M, float& L) {
+    M = s_m[0][qh];
 #pragma unroll
     for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][qh]);
     float4 y = make_float4(0, 0, 0, 0);
-    float L = 0.0f;
+    L = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float al = __builtin_amdgcn_exp2f(s_m[w][qh] - M);
       L = __builtin_fmaf(s_l[w][qh], al, L);
       add_scaled(y, *reinterpret_cast<const float4*>(&s_o[w][qh][4 * d4]), al);
     }
+    return y;
+  };
+  auto put = [&](int qh, int d4, float M, float L, const float4& y) {
     const size_t row = static_cast<size_t>(r) * a.Hq + h0 + qh;
     if (whole) {
       finish_row(a, row, d4, M, L, y);
@@ -346,6 +353,44 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
       reinterpret_cast<float4*>(a.part)[part * (D / 4) + d4] = y;
       if (d4 == 0) part_stats(a, sp)[part] = make_float2(M, L);
     }
+  };
+  float M, L;
+  bool odd = false;
+  for (int i = threadIdx.x; i < gq * (D / 4); i += 64 * W) {
+    const int qh = i / (D / 4), d4 = i % (D / 4);
+    const float4 y = joined(qh, d4, M, L);
+    odd |= is_nan(y.x + y.y + y.z + y.w);
+    put(qh, d4, M, L, y);
+  }
+  if (!odd) return;
+  // NaN where l is none: the sum of the attended values that are not finite
+  for (int i = threadIdx.x; i < gq * (D / 4); i += 64 * W) {
+    const int qh = i / (D / 4), d4 = i % (D / 4);
+    float4 y = joined(qh, d4, M, L);
+    if (!is_nan(y.x + y.y + y.z + y.w) || is_nan(L)) continue;
+    float sum[4] = {0, 0, 0, 0};
+    for (int tok = max(first, begin); tok < end; ++tok) {
+      const int page = page_of(tok);
+      if (page < 0) continue;
+      const size_t at = row_of(page, tok) * D;
+      float some[4];
+      bool any = false;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float w = half_lo<F16>(a.v[at + 4 * d4 + x]);
+        some[x] = w - w == 0.0f ? 0.0f : w;
+        any |= w - w != 0.0f;
+      }
+      if (!any) continue;
+      const uint16_t* qr = a.q + r * a.q_stride + static_cast<size_t>(h0 + qh) * D;
+      float dot = 0.0f;
+      for (int j = 0; j < D; ++j) dot = __builtin_fmaf(half_lo<F16>(qr[j]), half_lo<F16>(a.k[at + j]), dot);
+      const float factor = dot * scale == -INFINITY ? 0.0f : 1.0f;  // a probability of 0 makes it NaN
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum[x] += some[x] * factor;
+    }
+    auto pick = [](float v, float w) { return is_nan(v) && w != 0.0f ? w : v; };
+    put(qh, d4, M, L, make_float4(pick(y.x, sum[0]), pick(y.y, sum[1]), pick(y.z, sum[2]), pick(y.w, sum[3])));
   }
 }
 

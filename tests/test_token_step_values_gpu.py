@@ -147,3 +147,24 @@ def test_attn_scores_of_minus_infinity(dtype, L, D):
     y, lse = attend(q, k, v, [L, L], 16, "f32", scale=D ** -0.5)
     assert torch.equal(y[0], ref[0][0]) and torch.equal(lse[0], ref[1][0])
     assert (y[1] == 0).all() and (lse[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "f32"), ("f16", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("L,D", LENGTHS)
+def test_attn_infinite_values(dtype, out, L, D):
+    """An infinite value that is attended makes its dimension infinite, with its
+    sign; both signs, or a NaN, make it NaN; the other dimensions do not change."""
+    q, k, v = spread(3, L, 6, 2, D, dtype, L + D)
+    lens = [L, L - 1, L - 5]
+    want, lse = attend(q, k, v, lens, 16, out, scale=D ** -0.5)
+    inf = float("inf")
+    v[0, L // 3, 0, 3], v[0, L // 2, 1, 9], v[0, 0, 1, D - 1] = inf, -inf, inf
+    v[1, L - 2, 0, 0], v[1, 1, 0, 0], v[1, 2, 0, 1], v[1, L // 2, 0, 1] = inf, -inf, inf, inf
+    v[2, 0, 1, 40], v[2, 0, 1, 41] = float("nan"), -inf
+    want[0, :3, 3], want[0, 3:, 9], want[0, 3:, D - 1] = inf, -inf, inf
+    want[1, :3, 0], want[1, :3, 1] = float("nan"), inf
+    want[2, 3:, 40], want[2, 3:, 41] = float("nan"), -inf
+    y, lse2 = attend(q, k, v, lens, 16, out, scale=D ** -0.5)
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(y.nan_to_num(5.0, inf, -inf), want.nan_to_num(5.0, inf, -inf))
+    assert torch.equal(lse, lse2)
