@@ -578,7 +578,9 @@ sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, i
  * weight of the quantized linears, y [M][N] of out_dtype.  x * dinv is rounded
  * to fp32; it meets the matrix cores as bf16 parts whose sum holds 16
  * significant bits of it for 16-bit outputs and all 24 for fp32 (x itself
- * where dinv is NULL), products are exact and sums fp32.  Requires M <= 64
+ * where dinv is NULL), products are exact and sums fp32 (a sum that is not
+ * finite, as with an infinite x, is formed again in fp32 product by product:
+ * an infinity or NaN as the formula has it).  Requires M <= 64
  * (else SQ_ERR_UNSUPPORTED).  No workspace. */
 sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const sq_weight* w, void* y,
                           int32_t out_dtype, hipStream_t stream);

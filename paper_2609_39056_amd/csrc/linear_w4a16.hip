@@ -120,21 +120,55 @@ __device__ __forceinline__ void add_block(Fragment fragment, const Block<NT>& bl
   }
 }
 
+// y[m][n] without the bias as the formula reads, one product after the other.
+__device__ float plain_sum(const LinearArgs& a, int m, int n) {
+  const uint32_t* codes = reinterpret_cast<const uint32_t*>(a.qw + static_cast<size_t>(n) * (a.K / 2));
+  const uint16_t* x = a.x + static_cast<size_t>(m) * a.K;
+  float y = 0.0f;
+  for (int k0 = 0; k0 < a.K; k0 += 8) {
+    const float step = f16_to_f32(a.w_scale[static_cast<size_t>(k0 / a.w_group) * a.N + n]);
+    const uint32_t p = codes[k0 / 8];
+    for (int i = 0; i < 8; ++i) {
+      const int code = static_cast<int>(p << (28 - 8 * (i & 3) - 4 * (i >> 2))) >> 28;
+      const float v = bf16_to_f32(x[k0 + i]);
+      y = __builtin_fmaf(a.dinv != nullptr ? v * a.dinv[k0 + i] : v, static_cast<float>(code) * step, y);
+    }
+  }
+  return y;
+}
+
 // Adds the waves' sums (tile rows m * np .. + np make output row m0 + m), bias,
-// store.
+// store.  The parts of an infinite x~ (or of one past bf16's range) and code + 8
+// beside -8 leave NaN or infinities that its products do not have: such a sum is
+// formed again.
 template <int NT>
 __device__ __forceinline__ void finish(const LinearArgs& a, const float* sums, int waves, int tile_rows, int np, int m0,
                                        int rows, int n0) {
-  for (int i = threadIdx.x; i < rows * 16 * NT; i += blockDim.x) {
-    const int m = i / (16 * NT), t = (i / 16) % NT, c = i % 16, n = n0 + 16 * t + c;
-    const float bias = a.bias != nullptr ? bf16_to_f32(a.bias[n]) : 0.0f;
+  auto sum_of = [&](int i) {
+    const int m = i / (16 * NT), t = (i / 16) % NT, c = i % 16;
     float y = 0.0f;
     for (int u = 0; u < np; ++u) {
       const float* p = sums + (t * tile_rows + m * np + u) * 16 + c;
 #pragma unroll 4
       for (int w = 0; w < waves; ++w) y += p[w * NT * tile_rows * 16];
     }
-    store_out(a.y, static_cast<size_t>(m0 + m) * a.N + n, a.bias != nullptr ? y + bias : y, a.out_dtype);
+    return y;
+  };
+  auto put = [&](int i, float y) {
+    const int m = m0 + i / (16 * NT), n = n0 + 16 * ((i / 16) % NT) + i % 16;
+    if (a.bias != nullptr) y += bf16_to_f32(a.bias[n]);
+    store_out(a.y, static_cast<size_t>(m) * a.N + n, y, a.out_dtype);
+  };
+  bool odd = false;
+  for (int i = threadIdx.x; i < rows * 16 * NT; i += blockDim.x) {
+    const float y = sum_of(i);
+    odd |= y - y != 0.0f;
+    put(i, y);
+  }
+  if (!odd) return;
+  for (int i = threadIdx.x; i < rows * 16 * NT; i += blockDim.x) {
+    const float y = sum_of(i);
+    if (y - y != 0.0f) put(i, plain_sum(a, m0 + i / (16 * NT), n0 + 16 * ((i / 16) % NT) + i % 16));
   }
 }
 

@@ -168,3 +168,72 @@ def test_attn_infinite_values(dtype, out, L, D):
     assert torch.equal(torch.isnan(y), torch.isnan(want))
     assert torch.equal(y.nan_to_num(5.0, inf, -inf), want.nan_to_num(5.0, inf, -inf))
     assert torch.equal(lse, lse2)
+
+
+# ------------------------------------------------------------------ linear
+def packed(codes, step, group, bias=None):
+    """Codes int [N, K], steps [K / group, N] -> the weight on the device."""
+    N, K = codes.shape
+    c = (codes & 15).view(N, K // 8, 2, 4)
+    qw = (c[:, :, 0] | (c[:, :, 1] << 4)).to(torch.uint8).reshape(N, K // 2)
+    return B.Weight(qw.cuda(), step.half().cuda(), group, None if bias is None else bias.cuda())
+
+
+ROWS = [(1, 1280, 64), (3, 1280, 320), (5, 640, 4160), (16, 1280, 320), (20, 1280, 5120), (64, 256, 8256)]
+
+
+@pytest.mark.parametrize("M,K,N", ROWS)
+@pytest.mark.parametrize("use_d", [True, False])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_linear_infinite_rows(M, K, N, use_d, out):
+    """An infinite activation gives what its products do: an infinity with the
+    code's sign, NaN where the code is 0 or two of them have both signs; a NaN
+    gives NaN.  The other rows do not change."""
+    g = torch.Generator().manual_seed(M + N)
+    codes = torch.randint(-7, 8, (N, K), generator=g)
+    step = torch.rand((K // 128, N), generator=g) + 0.1
+    x = torch.randn((M, K), generator=g).to(torch.bfloat16)
+    dinv = torch.rand((K,), generator=g) + 0.5 if use_d else None
+    bias = torch.randn((N,), generator=g).to(torch.bfloat16)
+    W = packed(codes, step, 128, bias)
+
+    def run():
+        y = torch.full((M, N), 77.0, dtype=DT[out], device="cuda")
+        B.sq_linear_w4a16(x.cuda(), None if dinv is None else dinv.cuda(), W, y, OUT[out])
+        return y.cpu()
+
+    want = run()
+    inf = float("inf")
+    changed = {0: [(0, inf)], M // 2: [(130, -inf), (K - 1, inf)], M - 1: [(7, inf), (K - 5, inf)]}
+    if M > 4:
+        changed[1] = [(99, float("nan"))]
+    for m, at in changed.items():
+        x[m] = torch.randn((K,), generator=g).to(torch.bfloat16)
+        row = torch.zeros((N,))
+        for k, val in at:
+            x[m, k] = val
+            row = row + val * codes[:, k].float()
+        want[m] = row.to(DT[out])
+    y = run()
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(y.nan_to_num(5.0, inf, -inf), want.nan_to_num(5.0, inf, -inf))
+
+
+@pytest.mark.parametrize("M", [1, 2, 20])
+def test_linear_largest_values(M):
+    """Activations near the type's largest and a scaling that takes them past it
+    stay what fp32 makes of them."""
+    K, N = 256, 64
+    codes = torch.zeros((N, K), dtype=torch.long)
+    codes[:, 3], codes[:, 200] = torch.arange(N) % 8 - 1, 1
+    W = packed(codes, torch.full((2, N), 2.0 ** -10), 128)
+    x = torch.zeros((M, K), dtype=torch.bfloat16)
+    x[:, 3], x[:, 200] = 3.3e38, 1.0
+    y = torch.empty((M, N), device="cuda")
+    for d in (3.4e38 / x[0, 3].item(), 1.0, 0.5):  # the first is past bf16's range, within fp32's
+        dinv = torch.full((K,), d)
+        B.sq_linear_w4a16(x.cuda(), dinv.cuda(), W, y, B.SQ_OUT_F32)
+        want = ((x.float() * dinv).double() @ (codes.double() * 2.0 ** -10).t())
+        assert torch.isfinite(want).all()
+        # two products, each good to some units of the 15 |x~| that a code is met with
+        assert ((y.cpu().double() - want).abs() <= 64 * U * 15 * 2.0 ** -10 * 3.4e38 * d).all()
