@@ -539,7 +539,9 @@ sq_status sq_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_
 
 /* Bytes of device workspace for sq_attn_paged (partial results of histories
  * split over workgroups; no initialization needed), at least 256; 0 for
- * invalid arguments.  Host-only. */
+ * invalid arguments.  They serve every call with as many requests or fewer,
+ * max_kv_len as large or smaller and any window: one workspace for the largest
+ * batch is enough.  Host-only. */
 size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv, int32_t max_kv_len);
 
 /* Attention of one query token per request over the paged cache: with n =

@@ -545,7 +545,7 @@ void launch_dim(const AttnArgs& a, const AttnSplit& sp, hipStream_t s) {
 }  // namespace
 
 size_t attn_partial_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t max_kv_len) {
-  return attn_part_bytes(R, Hq, D, attn_most_splits(attn_heads(R, Hq, Hk), max_kv_len));
+  return attn_part_bytes(1, Hq, D, attn_most_parts(R, attn_heads(1, Hq, Hk), max_kv_len));
 }
 
 hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s) {

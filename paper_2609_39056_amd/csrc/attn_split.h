@@ -35,7 +35,11 @@ inline int64_t attn_heads(int32_t R, int32_t Hq, int32_t Hk) {
   return static_cast<int64_t>(R) * Hk * ((Hq / Hk + kAttnQTile - 1) / kAttnQTile);
 }
 inline int64_t attn_wanted(int64_t heads) { return std::max<int64_t>(1, 2048 / std::max<int64_t>(1, heads)); }
-inline bool attn_whole(int64_t heads, int64_t span) { return span <= (heads >= 512 ? kAttnWhole : heads >= 192 ? 640 : 384); }
+// So many heads or more leave a span whole (INT64_MAX: no number of them).
+inline int64_t attn_whole_from(int64_t span) {
+  return span <= 384 ? 0 : span <= 640 ? 192 : span <= kAttnWhole ? 512 : INT64_MAX;
+}
+inline bool attn_whole(int64_t heads, int64_t span) { return heads >= attn_whole_from(span); }
 // Whether a workgroup is a single wave: for one tile, and for two where the
 // heads fill the CUs several times over (2160 heads of up to 24 tokens 9.3 us,
 // with four waves 14.5; 4000 of 64 17.7 and 26.2; but 160 of 64 7.4 and 6.5, and
@@ -53,12 +57,25 @@ inline AttnSplit attn_split(int64_t heads, int64_t span) {
   return {static_cast<int32_t>(chunk), static_cast<int32_t>((span + chunk - 1) / chunk)};
 }
 
+// Splits into the shortest chunks.
+inline int64_t attn_shortest_splits(int64_t longest) {
+  return std::max((longest + kAttnLeast - 1) / kAttnLeast,
+                  (std::min(longest, kAttnShort) + kAttnLeastShort - 1) / kAttnLeastShort);
+}
 // No span up to `longest` is split into more parts.
 inline int64_t attn_most_splits(int64_t heads, int64_t longest) {
   if (attn_whole(heads, longest)) return 1;
-  const int64_t least = std::max((longest + kAttnLeast - 1) / kAttnLeast,
-                                 (std::min(longest, kAttnShort) + kAttnLeastShort - 1) / kAttnLeastShort);
-  return std::max(std::min(attn_wanted(heads), least), (longest + kAttnMost - 1) / kAttnMost);
+  return std::max(std::min(attn_wanted(heads), attn_shortest_splits(longest)), (longest + kAttnMost - 1) / kAttnMost);
+}
+// Parts (requests x splits) that no batch of at most R requests, of `each`
+// heads, with spans up to `longest` has more of.  Fewer requests are split into
+// more: up to the largest batch that is split at all, r requests have the most
+// splits of r, or wanted splits that come to 2048 heads at most in all.
+inline int64_t attn_most_parts(int64_t R, int64_t each, int64_t longest) {
+  const int64_t from = attn_whole_from(longest);
+  if (from == 0 || R == 0) return 0;
+  const int64_t r = std::min(R, (from - 1) / each);
+  return std::max(r * attn_most_splits(r * each, longest), std::min(2048 / each, r * attn_shortest_splits(longest)));
 }
 
 // Bytes of the parts: head_dim values, a maximum and a sum each.

@@ -36,6 +36,7 @@ struct AttnArgs {
   int32_t R, Hq, Hk, D, max_pages, num_pages, page_shift, max_kv_len, window, out_dtype;
   float scale;
 };
+// for every batch of at most R requests of at most max_kv_len tokens
 size_t attn_partial_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t max_kv_len);
 hipError_t launch_attn_paged(const AttnArgs& a, bool f16, hipStream_t s);
 

@@ -237,3 +237,21 @@ def test_linear_largest_values(M):
         assert torch.isfinite(want).all()
         # two products, each good to some units of the 15 |x~| that a code is met with
         assert ((y.cpu().double() - want).abs() <= 64 * U * 15 * 2.0 ** -10 * 3.4e38 * d).all()
+
+
+# ------------------------------------------------------------------ the batch drains
+def test_attn_workspace_serves_smaller_batches():
+    """One workspace, sized for the largest batch, through a batch that gets
+    smaller and shorter: the same results as with one of its own."""
+    Hq, Hk, D, L = 16, 4, 64, 1000
+    q, k, v = spread(130, L, Hq, Hk, D, "bf16", 3)
+    kv = B.KVCache(*(t.view(130 * L // 8, 8, Hk, D).transpose(1, 2).contiguous().cuda() for t in (k, v)))
+    table = torch.arange(130 * L // 8, dtype=torch.int32, device="cuda").view(130, L // 8)
+    ws = B.alloc_attn_workspace(130, Hq, kv, L)
+    q = q.cuda()
+    for R, n in ((130, 1000), (64, 1000), (40, 900), (24, 700), (7, 500), (1, 385)):
+        lens = torch.full((R,), n, dtype=torch.int32, device="cuda")
+        out = [torch.full((R, Hq, D), 77.0, device="cuda") for _ in range(2)]
+        for o, w in zip(out, (ws, B.alloc_attn_workspace(R, Hq, kv, n))):
+            B.sq_attn_paged(q[:R], kv, table[:R], lens, n, 0, 0.125, o, B.SQ_OUT_F32, None, w)
+        assert torch.equal(*out) and not (out[0] == 77.0).any()
