@@ -113,6 +113,16 @@ class sq_rope_params(ctypes.Structure):
     ]
 
 
+class _int32(ctypes.c_int32):
+    """An argument: ctypes alone passes the low 32 bits of a larger one."""
+
+    @classmethod
+    def from_param(cls, v):
+        if isinstance(v, int) and not -2**31 <= v < 2**31:
+            raise ValueError(f"{v} does not fit in 32 bits")
+        return ctypes.c_int32.from_param(v)
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _L = ctypes.c_int64
@@ -205,7 +215,7 @@ def lib() -> ctypes.CDLL:
         for name, (res, args) in _SIGS.items():
             f = getattr(L, name)
             f.restype = res
-            f.argtypes = args
+            f.argtypes = [_int32 if a is _I else a for a in args]
         L.sq_address = {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _SIGS}
         if _call is None:
             _call = _load_call()
