@@ -82,7 +82,7 @@ def cancelling(D, dtype, seed):
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("L,at", [(16, 0), (300, 96), (700, 640), (5000, 1536)])
 def test_attn_probabilities_are_whole(dtype, L, at):
-    """16-bit outputs too are sums over fp32 probabilities: a score's three
+    """16-bit outputs like fp32 ones are sums over fp32 probabilities: a score's three
     roundings in units of log 2 make 6 units of p (|s| < 1 and a factor of log2 e),
     the exponential 2, the parts 1, sixteen sums of exact products up to 18 and the
     quotient and rounding of a result that cancels to nothing none; 32 in all, of
@@ -99,11 +99,12 @@ def test_attn_probabilities_are_whole(dtype, L, at):
     vals[0, at:at + 16, 0] = torch.from_numpy(v).float()
     q = torch.zeros((1, 3, D))
     q[:, :, 0] = 1.0
-    y, _ = attend(q.to(dt), k.to(dt), vals.to(dt), [L], 16, dtype)
     want = (p[:, None] * v).sum(0) / p.sum()
     bound = bound / p.sum()
-    err = np.abs(y[0].double().numpy() - want[None])
-    assert (err <= bound + np.abs(want) * 2.0 ** -8).all(), f"{(err / bound).max():.3g} of the bound"
+    for out in (dtype, "f32"):
+        y, _ = attend(q.to(dt), k.to(dt), vals.to(dt), [L], 16, out)
+        err = np.abs(y[0].double().numpy() - want[None])
+        assert (err <= bound + np.abs(want) * 2.0 ** -8).all(), f"{out}: {(err / bound).max():.3g} of the bound"
 
 
 # ------------------------------------------------------------------ values that are not finite
@@ -255,3 +256,73 @@ def test_attn_workspace_serves_smaller_batches():
         for o, w in zip(out, (ws, B.alloc_attn_workspace(R, Hq, kv, n))):
             B.sq_attn_paged(q[:R], kv, table[:R], lens, n, 0, 0.125, o, B.SQ_OUT_F32, None, w)
         assert torch.equal(*out) and not (out[0] == 77.0).any()
+
+
+# ------------------------------------------------------------------ every token once
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("R,L,Hq,Hk,D,page,window", [
+    (3, 31, 2, 2, 64, 8, 0), (3, 1280, 2, 1, 128, 16, 0), (2, 5000, 8, 2, 96, 8, 0), (2, 5000, 32, 1, 128, 64, 1999),
+    (1, 20011, 4, 4, 192, 16, 0), (1, 66003, 32, 32, 64, 128, 0), (1, 66003, 2, 1, 256, 32, 65601), (70, 1300, 34, 2, 64, 16, 0),
+    (400, 64, 4, 4, 64, 8, 0), (300, 61, 6, 3, 96, 16, 7), (260, 48, 3, 3, 128, 8, 33), (200, 40, 4, 4, 192, 32, 0),
+    (200, 63, 5, 5, 256, 8, 20)])
+def test_attn_takes_every_token_once(R, L, Hq, Hk, D, page, window, dtype):
+    """Scores of 0 make every probability 1, and values of small integers make all
+    sums exact: a token left out, taken twice or from another place changes an
+    integer.  Out and lse carry a quotient, a logarithm and their roundings."""
+    g = torch.Generator().manual_seed(L)
+    lens = ([L, L - 1, max(0, L - 129), L // 2, 0, 33, 32, 1] + [(53 * r) % (L + 1) for r in range(R)])[:R]
+    k = torch.zeros((R, L, Hk, D), dtype=DT[dtype])
+    v = torch.randint(-3, 4, (R, L, Hk, D), generator=g, dtype=torch.int8)
+    q = torch.randn((R, Hq, D), generator=g)
+    y, lse = attend(q.to(DT[dtype]), k, v.to(DT[dtype]), lens, page, "f32", window=window)
+    for r, n in enumerate(lens):
+        first = max(0, n - window) if window else 0
+        total = v[r, first:n].sum(0).double().repeat_interleave(Hq // Hk, 0)
+        if n == 0:
+            assert (y[r] == 0).all() and (lse[r] == -math.inf).all()
+            continue
+        assert ((y[r].double() * (n - first) - total).abs() <= 4 * U * total.abs()).all(), (r, n)
+        # log2 to an ulp, of the sum in the kernel's units (f16: probabilities times 2^11),
+        # its product with ln 2 (rounded) and the result's rounding
+        size = math.log(n - first) + (11 * math.log(2) if dtype == "f16" else 0.0)
+        assert ((lse[r].double() - math.log(n - first)).abs() <= 6 * U * max(1.0, size)).all(), (r, n)
+
+
+# ------------------------------------------------------------------ norm and rotation of prompts
+@pytest.mark.parametrize("T", [511, 512, 513])
+@pytest.mark.parametrize("Hq,Hk,D,rot", [(33, 11, 128, 128), (40, 8, 128, 64), (12, 12, 192, 96), (5, 5, 96, 96),
+                                         (24, 7, 256, 256), (70, 35, 64, 64), (1, 1, 64, 0)])
+def test_rope_of_prompts(T, Hq, Hk, D, rot):
+    """From 512 tokens on a workgroup takes all heads of a token in several rounds,
+    queries, keys and values in turn, the last one ragged; below it one round."""
+    from test_token_step_gpu import check_rope, rope_case
+
+    for dtype, inter, norm in (("bf16", False, True), ("f16", True, True), ("bf16", True, False)):
+        c = rope_case(T, Hq, Hk, D, rot, dtype, T + D + Hq, norm=norm)
+        n = c["shape"][0] * c["shape"][2]
+        skip = dict(skip_pos=((3, -1), (T - 2, 50)), skip_slot=((0, -1), (7, n), (T - 1, 2 ** 31 - 1))) if rot else {}
+        check_rope(c, T, Hq, Hk, D, dtype, inter, use_k_out=inter, **skip)
+
+
+# ------------------------------------------------------------------ a product at a time
+@pytest.mark.parametrize("M,K,N", ROWS)
+def test_linear_keeps_every_bit_of_a_scaled_row(M, K, N):
+    """fp32 outputs take all 24 bits of x * dinv.  One channel of a row is not 0 and
+    its codes are 7 or -7, so y is 7 x~ step: three parts, the sums with code + 8
+    and of the -8, their difference and the step's product come to at most
+    (3 * 2 (15 + 8)) / 7 + 2 = 22 units.  Two parts of these x~ leave more."""
+    g = torch.Generator().manual_seed(M * N)
+    # x~ in (1, 2) whose two leading bf16 parts miss at least 2^-18.4
+    cand = (1 + torch.rand((20000,), generator=g)).numpy()
+    _, rest = halves(cand, torch.bfloat16, 2)
+    cand = torch.from_numpy(cand[np.abs(rest) > 48 * U * cand])
+    dinv = cand[torch.arange(K) % cand.numel()]
+    codes = torch.where(torch.rand((N, K), generator=g) < 0.5, 7, -7)
+    W = packed(codes, torch.full((K // 128, N), 0.25), 128)
+    x = torch.zeros((M, K), dtype=torch.bfloat16)
+    at = torch.randint(0, K, (M,), generator=g)
+    x[torch.arange(M), at] = 1.0
+    y = torch.empty((M, N), device="cuda")
+    B.sq_linear_w4a16(x.cuda(), dinv.cuda(), W, y, B.SQ_OUT_F32)
+    want = dinv[at].double()[:, None] * codes[:, at].t().double() * 0.25
+    assert ((y.cpu().double() - want).abs() <= 22 * U * want.abs()).all()
