@@ -567,8 +567,9 @@ size_t sq_attn_workspace_bytes(int32_t num_requests, int32_t q_heads, const sq_k
  * 0 <= num_requests <= 65535; q_heads a multiple of num_heads, at most 1024;
  * 0 <= max_kv_len <= max_pages * page_size < 2^31; window >= 0 (0: none);
  * scale finite.  max_kv_len bounds the work that is launched: the longest
- * history, or its capacity in a captured graph.  q, out and workspace 16-byte
- * aligned. */
+ * history, or its capacity in a captured graph (one far above the lengths
+ * costs time).  q, out and workspace 16-byte aligned; outputs must not overlap
+ * inputs. */
 sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv,
                         const int32_t* table, int32_t max_pages, const int32_t* kv_len, int32_t max_kv_len,
                         int32_t window, float scale, void* out, int32_t out_dtype, float* lse, void* workspace,

@@ -25,8 +25,8 @@
 // NaN (and l is not) the infinities are summed by themselves at the end.
 //
 // Reading the keys and values goes at 5.2 to 5.9 TB/s where there is enough of
-// it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 165 us; two histories of
-// 131072: 117 to 130 us; a copy of 4 GiB runs at 4.8 TB/s).  Nontemporal loads
+// it (64 requests of 1024 to 8192 tokens, 8 heads of 128: 162 to 172 us; two histories
+// of up to 131072: 113 to 151 us; a copy of 4 GiB runs at 4.8 TB/s).  Nontemporal loads
 // are 2 to 13 % faster than cached ones, the most on long histories.  A call with
 // little to read is bound by its chain of loads (length, table entry, keys) and
 // one launch: 5 to 7 us.
@@ -123,7 +123,8 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
   constexpr int EW = E / 2;   // the same in dwords
   // The next tile's keys are loaded once this tile's scores are formed, its
   // values after the products (3 to 4 % at head dimension 128); at 256 the
-  // registers that takes leave one workgroup per CU (58 us, without 50).
+  // registers that takes leave one workgroup per CU (64 histories up to 8192, 8 heads
+  // on one: 91 us, without 66).
   constexpr bool kAhead = D < 256 && W > 1;
   constexpr int kPages = (W == 1 ? kAttnLone : kAttnWhole) / kMinPage + 1;  // of a chunk: one for each of as many threads
   static_assert(kPages <= 64 * W, "one table entry per thread");

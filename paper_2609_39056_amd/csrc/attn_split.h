@@ -7,11 +7,13 @@
 // query heads: 22.5 us whole, 25 in parts), and up to 1280 where the pairs alone
 // fill the CUs (768 with 1055 tokens: 37 us whole, 42 in parts; 512 with up to 700:
 // 25 and 26; 2000 with up to 1200: 104 and 106; but 1024 with up to 1000: 56 and 52).
-// Longer ones aim at 2048 workgroups in all, eight per CU, so that ragged batches
-// even out: 512 heads with 1024 to 8192 tokens take 171 us in chunks of 512, 178 in
-// 384, 169 in 640 or 768, but 512 with up to 4096 93, 95, 95 and 97.  Spans past
-// 65536 may take chunks of 1024 (two histories of 131072, 8 heads: 136 us, 142 in
-// chunks of 512: half the parts to join).
+// Longer ones take chunks that make 2048 workgroups in all, eight per CU, but of at
+// least 128 tokens (256 past 4096) and at most 512, which is what decides where there
+// is much to read and evens out ragged batches: 512 heads with 1024 to 8192 tokens
+// (8192 workgroups of 512) take 171 us, 178 in chunks of 384, 169 in 640 or 768, but
+// 512 with up to 4096 93, 95, 95 and 97.  Spans past 65536 may take chunks of 1024
+// (two histories of 131072, 8 heads: 136 us, 142 in chunks of 512: half the parts to
+// join).
 #pragma once
 
 #include <stdint.h>

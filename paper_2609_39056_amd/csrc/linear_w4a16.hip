@@ -6,7 +6,16 @@
 // a sum of NP bf16 parts (x itself without a channel scaling, 16 bits of
 // x * dinv for 16-bit outputs, all 24 for fp32 ones), products are exact and
 // sums fp32.  A code is met as code + 8 (widen_codes); the matrix cores also
-// take the block's -8 * sum_k x~, as one more operand of constants.
+// take the block's -8 * sum_k x~, as one more operand of constants, so that the
+// fp32 sums of a block are several times its products (16 rows of 13824 -> 5120
+// against 64 bits: 5.6e-7 relative, the plain fp32 product 9.7e-7).
+//
+// The two parts leave up to 2^-17 of a term: before the output's rounding (2^-9 or
+// 2^-12 of the result) several times what fp32 does, after it 1.1 to 1.2 % of the f16
+// and 0.2 % of the bf16 outputs are not the nearest value (plain fp32 0.2 to 0.5 and
+// 0.04 to 0.07 %; 16 rows of 2048 -> 2048 and 13824 -> 5120).  Three parts are 15 to
+// 30 % slower from three rows on (8 rows of 5120 -> 5120 12.8 us, two 10.9; 64 of
+// 5120 -> 13824 47.7 and 36.4).
 //
 // The work is reading the weights once.  A workgroup owns 16 NT output
 // channels; its waves take the 128-channel blocks of K in turn (a lane 16
@@ -234,8 +243,8 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
 // of four waves, two to a CU (36.0; unscaled 22.5, eight waves 25.6; but 64 rows of
 // 5120 -> 5120, unscaled, with CUs to spare 17.0 and 13.5).  With a
 // scaling and 16 rows what is left is the splitting of x~ in every workgroup, 7.5
-// vector operations a value (13824 -> 5120, fp32 out: 25 us, vector units 80 %
-// busy; 13.8 without).
+// vector operations a value (13824 -> 5120, fp32 out: 23.4 us, 25.0 on weights that
+// come from memory, vector units 74 % busy; 13.8 without).
 template <int NP, int NT, int RT, int NW>
 struct Ring {
   static constexpr int X = RT * 16 * 2 * kBlock;    // row r, 16-byte chunk k at r * 256 + 16 * (k ^ (r & 15))
