@@ -369,26 +369,43 @@ __global__ __launch_bounds__(64 * W, D <= 128 ? 2 : 1) void attn_kernel(AttnArgs
     const int qh = i / (D / 4), d4 = i % (D / 4);
     float4 y = joined(qh, d4, M, L);
     if (!is_nan(y.x + y.y + y.z + y.w) || is_nan(L)) continue;
+    const float was[4] = {y.x, y.y, y.z, y.w};
     float sum[4] = {0, 0, 0, 0};
-    for (int tok = max(first, begin); tok < end; ++tok) {
+    bool open = true;  // some dimension's sum may still change
+    for (int tok = max(first, begin); tok < end && open; ++tok) {
       const int page = page_of(tok);
       if (page < 0) continue;
       const size_t at = row_of(page, tok) * D;
-      float some[4];
-      bool any = false;
+      const uint2 raw = *reinterpret_cast<const uint2*>(a.v + at + 4 * d4);
+      const float w[4] = {half_lo<F16>(raw.x), half_hi<F16>(raw.x), half_lo<F16>(raw.y), half_hi<F16>(raw.y)};
+      bool odd_here = false, infinite = false;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const float w = half_lo<F16>(a.v[at + 4 * d4 + x]);
-        some[x] = w - w == 0.0f ? 0.0f : w;
-        any |= w - w != 0.0f;
+        odd_here |= w[x] - w[x] != 0.0f;
+        infinite |= fabsf(w[x]) == INFINITY;
       }
-      if (!any) continue;
-      const uint16_t* qr = a.q + r * a.q_stride + static_cast<size_t>(h0 + qh) * D;
-      float dot = 0.0f;
-      for (int j = 0; j < D; ++j) dot = __builtin_fmaf(half_lo<F16>(qr[j]), half_lo<F16>(a.k[at + j]), dot);
-      const float factor = dot * scale == -INFINITY ? 0.0f : 1.0f;  // a probability of 0 makes it NaN
+      if (!odd_here) continue;
+      float factor = 1.0f;  // or 0, which makes an infinity NaN: where the probability is 0
+      if (infinite) {
+        const uint4* qr = reinterpret_cast<const uint4*>(a.q + r * a.q_stride + static_cast<size_t>(h0 + qh) * D);
+        const uint4* kr = reinterpret_cast<const uint4*>(a.k + at);
+        float dot = 0.0f;
+#pragma unroll 1  // its registers are the kernel's
+        for (int j = 0; j < D / 8; ++j) {
+          float u[8], v8[8];
+          widen8<F16>(qr[j], u);
+          widen8<F16>(kr[j], v8);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) sum[x] += some[x] * factor;
+          for (int x = 0; x < 8; ++x) dot = __builtin_fmaf(u[x], v8[x], dot);
+        }
+        if (dot * scale == -INFINITY) factor = 0.0f;
+      }
+      open = false;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (w[x] - w[x] != 0.0f) sum[x] += w[x] * factor;
+        open |= is_nan(was[x]) && !is_nan(sum[x]);
+      }
     }
     auto pick = [](float v, float w) { return is_nan(v) && w != 0.0f ? w : v; };
     put(qh, d4, M, L, make_float4(pick(y.x, sum[0]), pick(y.y, sum[1]), pick(y.z, sum[2]), pick(y.w, sum[3])));

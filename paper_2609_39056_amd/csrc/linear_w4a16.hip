@@ -134,7 +134,7 @@ __device__ float plain_sum(const LinearArgs& a, int m, int n) {
   const uint32_t* codes = reinterpret_cast<const uint32_t*>(a.qw + static_cast<size_t>(n) * (a.K / 2));
   const uint16_t* x = a.x + static_cast<size_t>(m) * a.K;
   float y = 0.0f;
-  for (int k0 = 0; k0 < a.K; k0 += 8) {
+  for (int k0 = 0; k0 < a.K && y == y; k0 += 8) {  // NaN stays
     const float step = f16_to_f32(a.w_scale[static_cast<size_t>(k0 / a.w_group) * a.N + n]);
     const uint32_t p = codes[k0 / 8];
     for (int i = 0; i < 8; ++i) {

@@ -137,6 +137,22 @@ def test_attn_nan_that_is_read_is_not_an_empty_row(dtype, L, D):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("L,D", LENGTHS)
+def test_attn_infinite_values_of_probability_zero(dtype, L, D):
+    """0 times an infinity: a value whose key's score is -infinity."""
+    q, k, v = spread(2, L, 4, 2, D, dtype, L + 3)
+    q[:, :, 2] = 1.0
+    k[:, L // 2, 0, 2] = float("-inf")
+    want, _ = attend(q, k, v, [L, L], 16, "f32", scale=D ** -0.5)
+    v[0, L // 2, 0, 7], v[1, L // 2, 0, 7], v[1, 0, 0, 7] = float("inf"), float("-inf"), float("-inf")
+    v[1, 3, 0, 6] = float("inf")
+    want[:, :2, 7], want[1, :2, 6] = float("nan"), float("inf")
+    y, _ = attend(q, k, v, [L, L], 16, "f32", scale=D ** -0.5)
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    assert torch.equal(y.nan_to_num(5.0, math.inf, -math.inf), want.nan_to_num(5.0, math.inf, -math.inf))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("L,D", LENGTHS)
 def test_attn_scores_of_minus_infinity(dtype, L, D):
     """An attended key whose score is -infinity has probability 0; a row of
     nothing else is like one that attends nothing."""
