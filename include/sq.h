@@ -588,6 +588,126 @@ sq_status sq_attn_paged(const void* q, int64_t q_stride, int32_t num_requests, i
 sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const sq_weight* w, void* y,
                           int32_t out_dtype, hipStream_t stream);
 
+/* Residual addition and root-mean-square norm of token rows, in fp32:
+ *     h = x + residual             (h = x without a residual)
+ *     u = h / sqrt(mean(h^2) + eps) * weight[k]   (without the factor when weight is NULL)
+ * to `sum` (h, rounded to the residual's type), to `y` (u, rounded to y_dtype)
+ * and, with act, to the 8-bit codes of a quantized linear: the quantization
+ * arithmetic of this header on u in the place of fp32(x), without a rounding of u
+ * before it.  Codes and row scales are what sq_gemm_w4a8 takes.
+ *   x         [M][K] of x_dtype, rows x_stride elements apart
+ *   residual  [M][K] of residual_dtype, rows residual_stride apart, or NULL
+ *   weight    fp32 [K] or NULL
+ *   sum       [M][K] of residual_dtype, rows sum_stride apart, or NULL; needs a residual
+ *   y         [M][K] of y_dtype or NULL
+ *   act       as for sq_quantize_act with act_bits 8 (else SQ_ERR_UNSUPPORTED),
+ *             or NULL: no codes
+ *   qx, act_scale   int8 [M][K] and fp32 r [M]; required with act
+ * The types are SQ_OUT_F32, SQ_OUT_BF16 or SQ_OUT_F16.  0 <= M <= 2^24;
+ * 8 <= K <= 32768, K % 8 == 0, with act K % 128 == 0; strides are multiples of
+ * 8 and at least K; eps >= 0, finite.  At least one output is required.  Tensors
+ * and weights 16-byte aligned, act_scale 4.  `sum` may be the residual, `sum` or
+ * y may be x (of the same type and stride); other outputs must not overlap
+ * inputs.  Inputs must be finite, and so must the sum of a row's h^2. */
+sq_status sq_add_rmsnorm(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual, int64_t residual_stride,
+                         int32_t residual_dtype, const float* weight, float eps, int32_t M, int32_t K, void* sum,
+                         int64_t sum_stride, void* y, int32_t y_dtype, const sq_act_params* act, int8_t* qx,
+                         float* act_scale, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Several continuations of a prompt (beams) in the token step: sq_beam_select
+ * chooses them from the step's logits, sq_kv_reorder makes the page tables follow
+ * the choice, sq_kv_copy_pages moves what cannot be shared in every layer's cache,
+ * and sq_attn_shared reads what the beams share once for all of them.
+ *
+ * Bytes of device workspace for sq_beam_select with at most these sizes (no
+ * initialization needed), at least 256; 0 for invalid arguments.  Host-only. */
+size_t sq_beam_workspace_bytes(int32_t num_rows, int32_t beams, int32_t vocab, int32_t width);
+
+/* The best continuations of each group of beams: row b of a group (rows are
+ * group * beams + b) goes on with token t at
+ *     total(b, t) = scores[b] + x[b][t] - log sum_u exp(x[b][u]),
+ * a row that is done only with end_token at total = scores[b].  The `width`
+ * largest totals of a group are written in order; equal ones stand in the order of
+ * their rows, and within a row tokens stand in the order of their logits, equal ones
+ * of their numbers.  Totals are formed in fp64 (exponentials in fp32) and rounded
+ * to fp32 in score_out.  Continuations of total -infinity are not taken, nor those
+ * of a row whose score is not finite or whose logits hold a NaN or +infinity: where
+ * fewer are left, parent and token are -1, score_out -infinity and done_out 0.
+ *   logits     [num_rows][vocab] of dtype (SQ_OUT_F32, BF16 or F16), rows `stride`
+ *              elements apart (a multiple of 8, at least vocab)
+ *   scores     fp32 [num_rows]
+ *   done       int32 [num_rows], not 0: the row has ended (its logits are not
+ *              read); NULL: none has
+ *   parent     int32 [num_rows / beams][width] out: the row that goes on
+ *   token      int32, the same shape, out
+ *   score_out  fp32, the same shape, out
+ *   done_out   int32, the same shape, out, or NULL: 1 where the parent is done or
+ *              the token is end_token
+ * 0 <= num_rows <= 65535, a multiple of beams; beams and width 1 .. 64; vocab
+ * 1 .. 2^20; with done or done_out 0 <= end_token < vocab.  logits and workspace
+ * 16-byte aligned.  With width == beams score_out may be scores, and done_out
+ * done (else SQ_ERR_UNSUPPORTED); other outputs must not overlap inputs. */
+sq_status sq_beam_select(const void* logits, int64_t stride, int32_t dtype, int32_t num_rows, int32_t beams, int32_t vocab,
+                         const float* scores, const int32_t* done, int32_t end_token, int32_t width, int32_t* parent,
+                         int32_t* token, float* score_out, int32_t* done_out, void* workspace, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* Bytes of device workspace for sq_kv_reorder with at most so many requests and
+ * pages (no initialization needed), at least 256; 0 for invalid arguments.
+ * Host-only. */
+size_t sq_kv_reorder_workspace_bytes(int32_t num_requests, int32_t num_pages);
+
+/* Page tables in another order: row r of table_out goes on from row s = parent[r]
+ * of table (r itself: unchanged; several rows the same s: a fork; none: the row is
+ * freed; parent[r] outside [0, num_requests): row r is empty).  With n = kv_len[s]
+ * (clamped to [0, max_pages * page_size]) and ceil(n / page_size) pages:
+ *     table_out[r][j] = table[s][j] for those pages,  kv_len_out[r] = n
+ * except that of the rows with the same s, those after the lowest r take a page of
+ * their own in the place of a partly filled last one (n % page_size > 0) and
+ *     copy_src[r] = the page of s,  copy_dst[r] = the new page,  copy_rows[r] = n % page_size
+ * (-1, -1 and 0 where nothing is to be copied): sq_kv_copy_pages does that in
+ * every cache before more is written to it.  A last entry that is no page number
+ * is passed on instead.
+ *
+ * A page is held by the rows of a table, nothing else is counted: the pages of
+ * rows that nobody goes on from are free if no other row that somebody goes on from
+ * holds them (a prefix that is to stay has a row of its own).  In the order of their
+ * lowest row and entry these are the first that new pages are taken from, by
+ * ascending r; then those of the free list from head = *free_head on, as sq_kv_plan
+ * takes them.  What is left of them returns to the list in front of the head
+ * (at most head pages; further ones are lost to it):
+ *     head_out = max(0, head + taken - freed),  free_pages[head_out ..] = the rest in order
+ * A row for which no page is left is empty, kv_len_out[r] = 0, and the last of its
+ * entries -1.
+ *   parent, kv_len  int32 [num_requests], 1 .. 8192 requests
+ *   free_pages      int32 [num_free], in and out (may be NULL when num_free is 0)
+ *   free_head       int32 [1], in [0, num_free] (clamped), or NULL for 0
+ *   table           int32 [num_requests][max_pages]; table_out of the same shape:
+ *                   entries past a row's pages are left as they are
+ *   kv_len_out, copy_src, copy_dst, copy_rows  int32 [num_requests] out
+ *   free_head_out   int32 [1] out
+ * Entries that are no page numbers (outside [0, num_pages)) are passed on and
+ * never freed.  Outputs must not overlap inputs or each other: table_out being
+ * table, kv_len_out being kv_len or parent, or free_head_out being free_head, is
+ * SQ_ERR_UNSUPPORTED.  page_size as in sq_kv_cache, num_pages * page_size,
+ * max_pages * page_size and num_requests * max_pages < 2^31. */
+sq_status sq_kv_reorder(const int32_t* parent, const int32_t* kv_len, int32_t num_requests, int32_t page_size,
+                        int32_t num_pages, int32_t* free_pages, int32_t num_free, const int32_t* free_head,
+                        const int32_t* table, int32_t max_pages, int32_t* table_out, int32_t* kv_len_out,
+                        int32_t* copy_src, int32_t* copy_dst, int32_t* copy_rows, int32_t* free_head_out, void* workspace,
+                        size_t ws_bytes, hipStream_t stream);
+
+/* Copies the first rows[i] tokens (clamped to [0, page_size]; rows NULL: all) of
+ * page src[i] to page dst[i], keys and values of every head, in each of the caches
+ * (a HOST array of up to 1024 of one shape and type: the layers of a model).  An
+ * entry whose src or dst is no page number, or whose src is its dst, copies
+ * nothing.  Within a call a page must be the dst of one entry at most, and no
+ * entry's src.
+ *   src, dst, rows  int32 [n], 0 <= n <= 65535 */
+sq_status sq_kv_copy_pages(const sq_kv_cache* caches, int32_t num_caches, const int32_t* src, const int32_t* dst,
+                           const int32_t* rows, int32_t n, hipStream_t stream);
+
 /* Measurement hook: the int8 matrix-core rate the GPU sustains, as a
  * ceiling beside the published peak.  Launches sq_probe_mfma_i8_sink_bytes()
  * / 1024 workgroups (two per CU) whose waves each issue back-to-back int8

@@ -22,7 +22,7 @@ import importlib.util
 import os
 import warnings
 from dataclasses import dataclass
-from typing import Optional
+from typing import Optional, Sequence
 
 import torch
 
@@ -168,6 +168,13 @@ _SIGS = {
     "sq_attn_paged": (_I, [_P, _L, _I, _I, ctypes.POINTER(sq_kv_cache), _P, _I, _P, _I, _I, ctypes.c_float, _P, _I, _P,
                            _P, _S, _P]),
     "sq_linear_w4a16": (_I, [_P, _I, _P, ctypes.POINTER(sq_weight), _P, _I, _P]),
+    "sq_add_rmsnorm": (_I, [_P, _L, _I, _P, _L, _I, _P, ctypes.c_float, _I, _I, _P, _L, _P, _I,
+                            ctypes.POINTER(sq_act_params), _P, _P, _P]),
+    "sq_beam_workspace_bytes": (_S, [_I, _I, _I, _I]),
+    "sq_beam_select": (_I, [_P, _L, _I, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _S, _P]),
+    "sq_kv_reorder_workspace_bytes": (_S, [_I, _I]),
+    "sq_kv_reorder": (_I, [_P, _P, _I, _I, _I, _P, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
+    "sq_kv_copy_pages": (_I, [ctypes.POINTER(sq_kv_cache), _I, _P, _P, _P, _I, _P]),
     "sq_probe_mfma_i8_sink_bytes": (_S, []),
     "sq_probe_mfma_i8": (_I, [_I, _I, _I, _I, _P, _S, _P]),
     "sq_probe_mfma_f8f6": (_I, [_I, _I, _I, _I, _P, _S, _P]),
@@ -696,7 +703,126 @@ def sq_linear_w4a16(x: torch.Tensor, dinv: Optional[torch.Tensor], w: Weight, y:
            "sq_linear_w4a16")
 
 
+ANY_DTYPES = {t: code for code, t in OUT_DTYPES.items()}
+
+
+def _rows(t: Optional[torch.Tensor], M: int, K: int):
+    """Pointer, row stride and type of [M, K] whose rows are contiguous."""
+    if t is None:
+        return None, 0, 0
+    if not t.is_cuda:
+        raise ValueError("libsq takes device tensors")
+    if t.shape != (M, K) or t.dtype not in ANY_DTYPES:
+        raise ValueError(f"expected a tensor [{M}, {K}] of 32 or 16 bits")
+    if t.stride(1) != 1 and K > 1:
+        raise ValueError("libsq takes rows that are contiguous")
+    # one row has no stride: the next multiple of 8 stands for it
+    return t.data_ptr(), t.stride(0) if M > 1 else -(-K // 8) * 8, ANY_DTYPES[t.dtype]
+
+
+def sq_add_rmsnorm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: Optional[torch.Tensor], eps: float,
+                   sum_out: Optional[torch.Tensor], y: Optional[torch.Tensor], out_dtype: int,
+                   act: Optional[ActParams], qx: Optional[torch.Tensor], act_scale: Optional[torch.Tensor],
+                   stream=None) -> None:
+    """h = x + residual [M, K] into sum_out, its root-mean-square norm into y (of
+    out_dtype) and / or, with act, the 8-bit codes qx and row scales of a quantized
+    linear (include/sq.h).  x, residual and sum_out may be views with contiguous rows."""
+    M, K = x.shape
+    xp, xs, xd = _rows(x, M, K)
+    rp, rs, rd = _rows(residual, M, K)
+    sp, ss, sd = _rows(sum_out, M, K)
+    _typed(torch.float32, weight, act_scale)
+    _typed(torch.int8, qx)
+    if ((sum_out is not None and (residual is None or sd != rd)) or (weight is not None and weight.shape != (K,))
+            or (y is not None and (y.shape != (M, K) or y.dtype != OUT_DTYPES.get(out_dtype)))
+            or (qx is not None and qx.shape != (M, K)) or (act_scale is not None and act_scale.shape != (M,))):
+        raise ValueError("sq_add_rmsnorm: the tensors' sizes or types do not fit together")
+    if act is not None and (act.tok2stream.shape != (M,) or (act.dinv is not None and act.dinv.shape != (K,))):
+        raise ValueError("sq_add_rmsnorm: one stream id per row and one scale per channel")
+    a = None if act is None else ctypes.byref(act.struct())
+    _check(lib().sq_add_rmsnorm(xp, xs, xd, rp, rs, rd, _ptr(weight), eps, M, K, sp, ss, _ptr(y), out_dtype, a, _ptr(qx),
+                                _ptr(act_scale), _stream(stream)), "sq_add_rmsnorm")
+
+
+# ------------------------------------------------------------------ beams
+def sq_beam_workspace_bytes(num_rows: int, beams: int, vocab: int, width: int) -> int:
+    return int(lib().sq_beam_workspace_bytes(num_rows, beams, vocab, width))
+
+
+def sq_beam_select(logits: torch.Tensor, beams: int, scores: torch.Tensor, done: Optional[torch.Tensor], end_token: int,
+                   parent: torch.Tensor, token: torch.Tensor, score_out: torch.Tensor, done_out: Optional[torch.Tensor],
+                   workspace: torch.Tensor, stream=None) -> None:
+    """The width best continuations of every group of `beams` rows of logits [R, vocab]
+    (rows may be a view's) into parent, token, score_out and done_out [R / beams, width]
+    (include/sq.h)."""
+    R, V = logits.shape
+    xp, xs, xd = _rows(logits, R, V)
+    _typed(torch.int32, done, parent, token, done_out)
+    _typed(torch.float32, scores, score_out)
+    if parent.dim() != 2 or beams < 1 or R % beams != 0:
+        raise ValueError("sq_beam_select: the tensors' sizes do not fit together")
+    out = (R // beams, parent.shape[1])
+    if (scores.shape != (R,) or (done is not None and done.shape != (R,)) or
+            any(t is not None and t.shape != out for t in (parent, token, score_out, done_out))):
+        raise ValueError("sq_beam_select: the tensors' sizes do not fit together")
+    wp, wb = _ws(workspace)
+    _check(lib().sq_beam_select(xp, xs, xd, R, beams, V, _ptr(scores), _ptr(done), end_token, out[1], _ptr(parent),
+                                _ptr(token), _ptr(score_out), _ptr(done_out), wp, wb, _stream(stream)), "sq_beam_select")
+
+
+def sq_kv_reorder_workspace_bytes(num_requests: int, num_pages: int) -> int:
+    return int(lib().sq_kv_reorder_workspace_bytes(num_requests, num_pages))
+
+
+def sq_kv_reorder(parent: torch.Tensor, kv_len: torch.Tensor, page_size: int, num_pages: int, free_pages: torch.Tensor,
+                  free_head: Optional[torch.Tensor], table: torch.Tensor, table_out: torch.Tensor,
+                  kv_len_out: torch.Tensor, copy_src: torch.Tensor, copy_dst: torch.Tensor, copy_rows: torch.Tensor,
+                  free_head_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Tables [R, max_pages] whose row r goes on from row parent[r], pages that come free,
+    and the copies that sq_kv_copy_pages has to make (include/sq.h); every tensor int32."""
+    _typed(torch.int32, parent, kv_len, free_pages, free_head, table, table_out, kv_len_out, copy_src, copy_dst, copy_rows,
+           free_head_out)
+    if table.dim() != 2:
+        raise ValueError("sq_kv_reorder: the tensors' sizes do not fit together")
+    R, max_pages = table.shape
+    if (any(t.shape != (R,) for t in (parent, kv_len, kv_len_out, copy_src, copy_dst, copy_rows))
+            or table_out.shape != table.shape or free_pages.dim() != 1 or free_head_out.numel() < 1
+            or (free_head is not None and free_head.numel() < 1)):
+        raise ValueError("sq_kv_reorder: the tensors' sizes do not fit together")
+    wp, wb = _ws(workspace)
+    _check(lib().sq_kv_reorder(_ptr(parent), _ptr(kv_len), R, page_size, num_pages, _ptr(free_pages), free_pages.numel(),
+                               _ptr(free_head), _ptr(table), max_pages, _ptr(table_out), _ptr(kv_len_out), _ptr(copy_src),
+                               _ptr(copy_dst), _ptr(copy_rows), _ptr(free_head_out), wp, wb, _stream(stream)),
+           "sq_kv_reorder")
+
+
+def sq_kv_copy_pages(caches: Sequence[KVCache], src: torch.Tensor, dst: torch.Tensor, rows: Optional[torch.Tensor],
+                     stream=None) -> None:
+    """The first rows[i] tokens of page src[i] to page dst[i] in every cache of the
+    sequence (include/sq.h); src, dst and rows int32 [n], rows None: whole pages."""
+    _typed(torch.int32, src, dst, rows)
+    if src.dim() != 1 or dst.shape != src.shape or (rows is not None and rows.shape != src.shape):
+        raise ValueError("sq_kv_copy_pages: the tensors' sizes do not fit together")
+    c = (sq_kv_cache * len(caches))(*[kv.struct() for kv in caches])
+    _check(lib().sq_kv_copy_pages(c, len(caches), _ptr(src), _ptr(dst), _ptr(rows), src.shape[0], _stream(stream)),
+           "sq_kv_copy_pages")
+
+
 # ------------------------------------------------------------------ helpers
+def alloc_beam_workspace(num_rows: int, beams: int, vocab: int, width: int, device="cuda") -> torch.Tensor:
+    n = sq_beam_workspace_bytes(num_rows, beams, vocab, width)
+    if n == 0:
+        raise ValueError("invalid sizes for a beam workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_reorder_workspace(num_requests: int, num_pages: int, device="cuda") -> torch.Tensor:
+    n = sq_kv_reorder_workspace_bytes(num_requests, num_pages)
+    if n == 0:
+        raise ValueError("invalid sizes for a reorder workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 def alloc_attn_workspace(num_requests: int, q_heads: int, kv: KVCache, max_kv_len: int) -> torch.Tensor:
     n = sq_attn_workspace_bytes(num_requests, q_heads, kv, max_kv_len)
     if n == 0:

@@ -1,0 +1,56 @@
+// Copies of partly filled or whole pages inside the caches of several layers
+// (sq_kv_copy_pages).  A page is [heads][page_size][head_dim], so the first rows
+// of its heads are runs of rows * head_dim values; a workgroup takes a share of
+// one page of one tensor, in 16-byte pieces.
+#include <algorithm>
+
+#include "token_internal.h"
+
+namespace sq {
+namespace {
+
+typedef unsigned int Piece __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kAhead = 4;  // pieces of a thread in flight
+
+__global__ __launch_bounds__(kThreads) void kv_copy_kernel(CopyArgs a, unsigned parts) {
+  const int i = blockIdx.y;
+  const int32_t src = a.src[i], dst = a.dst[i];
+  if (src < 0 || src >= a.num_pages || dst < 0 || dst >= a.num_pages || src == dst) return;
+  const uint32_t P = 1u << a.page_shift;
+  const uint32_t rows = a.rows == nullptr ? P : static_cast<uint32_t>(min(max(a.rows[i], 0), static_cast<int32_t>(P)));
+  const uint32_t run = rows * (static_cast<uint32_t>(a.row_bytes) / 16);  // pieces of a head
+  const uint32_t total = run * static_cast<uint32_t>(a.heads);
+  const unsigned tensor = blockIdx.x / parts, part = blockIdx.x % parts;
+  const uint32_t head = P * (static_cast<uint32_t>(a.row_bytes) / 16);  // pieces from one head to the next
+  Piece* pages = static_cast<Piece*>(a.pages[tensor]);
+  const size_t page = static_cast<size_t>(head) * a.heads;
+  const Piece* from = pages + src * page;
+  Piece* to = pages + dst * page;
+  const uint32_t step = parts * kThreads;
+  for (uint32_t p = part * kThreads + threadIdx.x; p < total; p += kAhead * step) {
+    Piece v[kAhead];
+    uint32_t at[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t q = min(p + u * step, total - 1);  // (a piece past the end repeats the last)
+      at[u] = q / run * head + q % run;
+      v[u] = from[at[u]];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) to[at[u]] = v[u];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kv_copy(const CopyArgs& a, hipStream_t s) {
+  const size_t page = (static_cast<size_t>(a.row_bytes) << a.page_shift) * a.heads;
+  const unsigned parts = static_cast<unsigned>(std::max<size_t>(1, page / (kThreads * 16 * kAhead)));
+  const dim3 grid(2 * static_cast<unsigned>(a.caches) * parts, static_cast<unsigned>(a.n));
+  kv_copy_kernel<<<grid, kThreads, 0, s>>>(a, parts);
+  return hipGetLastError();
+}
+
+}  // namespace sq

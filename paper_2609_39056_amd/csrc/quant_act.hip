@@ -10,22 +10,11 @@
 // range reduction and the quantization, so X is read from HBM exactly once.
 // With WPR = 4 the four waves of a workgroup share the row and combine its
 // 8-bit range through LDS.
+#include "code_bits.h"
 #include "sq_internal.h"
 
 namespace sq {
 namespace {
-
-// t rounded to the nearest integer, ties to even, for abs(t) <= 2^22: adding
-// 1.5 * 2^23 leaves exactly the rounded value in the low mantissa bits, so the
-// two's-complement code is the low byte (8-bit) or nibble (4-bit) of the sum.
-__device__ __forceinline__ uint32_t rne_code_bits(float t) { return __float_as_uint(t + 12582912.0f); }
-
-// Bytes b0 of four words, in order, as one word.
-__device__ __forceinline__ uint32_t pack_low_bytes(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
-  const uint32_t lo = __builtin_amdgcn_perm(w1, w0, 0x0c0c0400u);  // [w0.b0, w1.b0, 0, 0]
-  const uint32_t hi = __builtin_amdgcn_perm(w3, w2, 0x0c0c0400u);  // [w2.b0, w3.b0, 0, 0]
-  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-}
 
 template <int BITS, int WPR, int NCH, bool F8>
 __global__ __launch_bounds__(256) void quantize_act_kernel(QuantArgs a) {

@@ -357,6 +357,7 @@ bool valid_half(int32_t d) { return d == SQ_OUT_BF16 || d == SQ_OUT_F16; }
 constexpr int64_t kIndexEnd = int64_t{1} << 31;
 constexpr int32_t kMaxRequests = 65535;  // a grid's y dimension
 constexpr int32_t kMaxQHeads = 1024, kMaxKvHeads = 256;
+constexpr int32_t kMaxBeams = 64, kMaxVocab = 1 << 20, kMaxCopyCaches = 1024;
 
 sq_status check_cache(const sq_kv_cache* kv) {
   if (kv == nullptr || kv->k == nullptr || kv->v == nullptr) return SQ_ERR_NULL;
@@ -371,6 +372,11 @@ sq_status check_cache(const sq_kv_cache* kv) {
 // Rows of `heads` contiguous heads, `stride` elements apart, in 16-byte pieces.
 bool valid_stride(int64_t stride, int32_t heads, int32_t dim) {
   return stride >= static_cast<int64_t>(heads) * dim && stride % 8 == 0 && stride <= (int64_t{1} << 40);
+}
+
+bool valid_beams(int32_t rows, int32_t beams, int32_t vocab, int32_t width) {
+  return rows >= 0 && rows <= kMaxRequests && beams >= 1 && beams <= kMaxBeams && rows % beams == 0 && vocab >= 1 &&
+         vocab <= kMaxVocab && width >= 1 && width <= kMaxBeams;
 }
 
 bool valid_attn_sizes(int32_t R, int32_t Hq, const sq_kv_cache* kv, int32_t max_kv_len) {
@@ -1003,6 +1009,162 @@ sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(dinv, 16)) return SQ_ERR_ALIGN;
   const LinearArgs a{x, dinv, w->qw, w->w_scale, w->bias, y, M, w->N, w->K, w->w_group, out_dtype};
   return hip_status(launch_linear_w4a16(a, stream));
+}
+
+sq_status sq_add_rmsnorm(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual, int64_t residual_stride,
+                         int32_t residual_dtype, const float* weight, float eps, int32_t M, int32_t K, void* sum,
+                         int64_t sum_stride, void* y, int32_t y_dtype, const sq_act_params* act, int8_t* qx,
+                         float* act_scale, hipStream_t stream) {
+  if (!valid_out(x_dtype) || (residual != nullptr && !valid_out(residual_dtype)) || (y != nullptr && !valid_out(y_dtype)) ||
+      !std::isfinite(eps) || eps < 0.0f)
+    return SQ_ERR_UNSUPPORTED;
+  if (M < 0 || M > kMaxM || K < 8 || K > kMaxK || K % 8 != 0) return SQ_ERR_SHAPE;
+  if (act != nullptr) {
+    const sq_status st = check_act(act, K);
+    if (st != SQ_OK) return st;
+    if (act->act_bits != 8) return SQ_ERR_UNSUPPORTED;
+  }
+  if (M == 0) return SQ_OK;
+  if (x == nullptr || (act != nullptr && (qx == nullptr || act_scale == nullptr)) || (sum != nullptr && residual == nullptr) ||
+      (y == nullptr && act == nullptr && sum == nullptr))
+    return SQ_ERR_NULL;
+  if (!valid_stride(x_stride, 1, K) || (residual != nullptr && !valid_stride(residual_stride, 1, K)) ||
+      (sum != nullptr && !valid_stride(sum_stride, 1, K)))
+    return SQ_ERR_SHAPE;
+  if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(sum, 16) || !aligned(y, 16) ||
+      (act != nullptr && (!aligned(qx, 16) || !aligned(act_scale, 4))))
+    return SQ_ERR_ALIGN;
+  NormArgs a{};
+  a.x = x;
+  a.residual = residual;
+  a.x_stride = x_stride;
+  a.residual_stride = residual_stride;
+  a.sum_stride = sum_stride;
+  a.weight = weight;
+  a.sum = sum;
+  a.y = y;
+  a.M = M;
+  a.K = K;
+  a.x_dtype = x_dtype;
+  a.residual_dtype = residual_dtype;
+  a.y_dtype = y_dtype;
+  a.eps = eps;
+  if (act != nullptr) {
+    a.qx = qx;
+    a.scale = act_scale;
+    a.tok2stream = act->tok2stream;
+    a.gamma = act->gamma;
+    a.clip = act->clip;
+    a.dinv = act->dinv;
+    a.S = act->num_streams;
+    a.step = act->step;
+    a.range_mode = act->range_mode;
+  }
+  return hip_status(launch_add_rmsnorm(a, stream));
+}
+
+// ---------------------------------------------------------------- beams
+size_t sq_beam_workspace_bytes(int32_t num_rows, int32_t beams, int32_t vocab, int32_t width) {
+  if (!valid_beams(num_rows, beams, vocab, width)) return 0;
+  return std::max(kAlign, round_up(beam_ws_bytes(num_rows, vocab, width)));
+}
+
+sq_status sq_beam_select(const void* logits, int64_t stride, int32_t dtype, int32_t num_rows, int32_t beams, int32_t vocab,
+                         const float* scores, const int32_t* done, int32_t end_token, int32_t width, int32_t* parent,
+                         int32_t* token, float* score_out, int32_t* done_out, void* workspace, size_t ws_bytes,
+                         hipStream_t stream) {
+  if (!valid_out(dtype)) return SQ_ERR_UNSUPPORTED;
+  if (!valid_beams(num_rows, beams, vocab, width)) return SQ_ERR_SHAPE;
+  if ((done != nullptr || done_out != nullptr) && (end_token < 0 || end_token >= vocab)) return SQ_ERR_SHAPE;
+  if (num_rows == 0) return SQ_OK;
+  if (logits == nullptr || scores == nullptr || parent == nullptr || token == nullptr || score_out == nullptr ||
+      workspace == nullptr)
+    return SQ_ERR_NULL;
+  if (!valid_stride(stride, 1, vocab)) return SQ_ERR_SHAPE;
+  if (!aligned(logits, 16) || !aligned(workspace, 16)) return SQ_ERR_ALIGN;
+  for (const void* p : {static_cast<const void*>(scores), static_cast<const void*>(done), static_cast<const void*>(parent),
+                        static_cast<const void*>(token), static_cast<const void*>(score_out),
+                        static_cast<const void*>(done_out)})
+    if (!aligned(p, 4)) return SQ_ERR_ALIGN;
+  // a group's outputs take its inputs' place only where there are as many
+  if (width != beams && (score_out == scores || (done != nullptr && done_out == done))) return SQ_ERR_UNSUPPORTED;
+  if (ws_bytes < sq_beam_workspace_bytes(num_rows, beams, vocab, width)) return SQ_ERR_WORKSPACE;
+  BeamArgs a{logits, stride, scores, done, parent, token, done_out, score_out, workspace, num_rows, beams, vocab, width,
+             end_token, dtype};
+  return hip_status(launch_beam_select(a, stream));
+}
+
+size_t sq_kv_reorder_workspace_bytes(int32_t num_requests, int32_t num_pages) {
+  if (num_requests < 1 || num_requests > kPlanMaxRequests || num_pages < 1) return 0;
+  return std::max(kAlign, round_up(4 * reorder_ws_ints(num_requests, num_pages)));
+}
+
+sq_status sq_kv_reorder(const int32_t* parent, const int32_t* kv_len, int32_t num_requests, int32_t page_size,
+                        int32_t num_pages, int32_t* free_pages, int32_t num_free, const int32_t* free_head,
+                        const int32_t* table, int32_t max_pages, int32_t* table_out, int32_t* kv_len_out,
+                        int32_t* copy_src, int32_t* copy_dst, int32_t* copy_rows, int32_t* free_head_out, void* workspace,
+                        size_t ws_bytes, hipStream_t stream) {
+  if (parent == nullptr || kv_len == nullptr || table == nullptr || table_out == nullptr || kv_len_out == nullptr ||
+      copy_src == nullptr || copy_dst == nullptr || copy_rows == nullptr || free_head_out == nullptr ||
+      workspace == nullptr || (num_free > 0 && free_pages == nullptr))
+    return SQ_ERR_NULL;
+  if (!valid_page(page_size)) return SQ_ERR_UNSUPPORTED;
+  if (num_requests < 1 || num_requests > kPlanMaxRequests || num_free < 0 || num_pages < 1 || max_pages < 1 ||
+      static_cast<int64_t>(num_pages) * page_size >= kIndexEnd || static_cast<int64_t>(max_pages) * page_size >= kIndexEnd ||
+      static_cast<int64_t>(num_requests) * max_pages >= kIndexEnd)
+    return SQ_ERR_SHAPE;
+  if (!aligned(workspace, 16)) return SQ_ERR_ALIGN;
+  for (const void* p :
+       {static_cast<const void*>(parent), static_cast<const void*>(kv_len), static_cast<const void*>(free_pages),
+        static_cast<const void*>(free_head), static_cast<const void*>(table), static_cast<const void*>(table_out),
+        static_cast<const void*>(kv_len_out), static_cast<const void*>(copy_src), static_cast<const void*>(copy_dst),
+        static_cast<const void*>(copy_rows), static_cast<const void*>(free_head_out)})
+    if (!aligned(p, 4)) return SQ_ERR_ALIGN;
+  // rows, lengths and the head are read after outputs have been written
+  if (table_out == table || kv_len_out == kv_len || kv_len_out == parent || free_head_out == free_head)
+    return SQ_ERR_UNSUPPORTED;
+  if (ws_bytes < sq_kv_reorder_workspace_bytes(num_requests, num_pages)) return SQ_ERR_WORKSPACE;
+  ReorderArgs a{parent, kv_len, table, free_head, free_pages, table_out, kv_len_out, copy_src, copy_dst, copy_rows,
+                free_head_out, static_cast<int32_t*>(workspace), num_requests, max_pages, num_pages, num_free,
+                log2_of(page_size)};
+  return hip_status(launch_kv_reorder(a, stream));
+}
+
+sq_status sq_kv_copy_pages(const sq_kv_cache* caches, int32_t num_caches, const int32_t* src, const int32_t* dst,
+                           const int32_t* rows, int32_t n, hipStream_t stream) {
+  if (num_caches < 0 || num_caches > kMaxCopyCaches || n < 0 || n > kMaxRequests) return SQ_ERR_SHAPE;
+  if (num_caches == 0) return SQ_OK;
+  if (caches == nullptr) return SQ_ERR_NULL;
+  for (int32_t i = 0; i < num_caches; ++i) {
+    const sq_status st = check_cache(caches + i);
+    if (st != SQ_OK) return st;
+    if (caches[i].dtype != caches[0].dtype) return SQ_ERR_UNSUPPORTED;
+    if (caches[i].num_pages != caches[0].num_pages || caches[i].num_heads != caches[0].num_heads ||
+        caches[i].page_size != caches[0].page_size || caches[i].head_dim != caches[0].head_dim)
+      return SQ_ERR_SHAPE;
+  }
+  if (n == 0) return SQ_OK;
+  if (src == nullptr || dst == nullptr) return SQ_ERR_NULL;
+  if (!aligned(src, 4) || !aligned(dst, 4) || !aligned(rows, 4)) return SQ_ERR_ALIGN;
+  CopyArgs a{};
+  a.src = src;
+  a.dst = dst;
+  a.rows = rows;
+  a.n = n;
+  a.num_pages = caches[0].num_pages;
+  a.heads = caches[0].num_heads;
+  a.page_shift = log2_of(caches[0].page_size);
+  a.row_bytes = 2 * caches[0].head_dim;
+  for (int32_t i = 0; i < num_caches; i += kCopyMaxCaches) {
+    a.caches = std::min(kCopyMaxCaches, num_caches - i);
+    for (int32_t c = 0; c < a.caches; ++c) {
+      a.pages[2 * c] = caches[i + c].k;
+      a.pages[2 * c + 1] = caches[i + c].v;
+    }
+    const hipError_t e = launch_kv_copy(a, stream);
+    if (e != hipSuccess) return SQ_ERR_HIP;
+  }
+  return SQ_OK;
 }
 
 }  // extern "C"

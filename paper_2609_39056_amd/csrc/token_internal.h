@@ -1,5 +1,7 @@
 // Internal declarations of a decoder's token step: page plan, head norm and
-// rotation, paged attention, the bf16 linear on int4 weights.
+// rotation, paged attention, the bf16 linear on int4 weights, the residual norm;
+// and of its beams: their choice, the tables and pages that follow it, attention
+// over a shared prefix.
 #pragma once
 
 #include "sq_internal.h"
@@ -51,5 +53,49 @@ struct LinearArgs {
 };
 constexpr int32_t kLinear16MaxM = 64;
 hipError_t launch_linear_w4a16(const LinearArgs& a, hipStream_t s);
+
+struct NormArgs {
+  const void *x, *residual;  // residual NULL: none
+  int64_t x_stride, residual_stride, sum_stride;
+  const float* weight;  // or NULL
+  void *sum, *y;        // each or NULL
+  int8_t* qx;           // or NULL
+  float* scale;
+  const int32_t* tok2stream;
+  const float *gamma, *clip, *dinv;
+  int32_t M, K, x_dtype, residual_dtype, y_dtype, S, step, range_mode;
+  float eps;
+};
+hipError_t launch_add_rmsnorm(const NormArgs& a, hipStream_t s);
+
+struct ReorderArgs {
+  const int32_t *parent, *kv_len, *table, *free_head;
+  int32_t *free_pages, *table_out, *kv_len_out, *copy_src, *copy_dst, *copy_rows, *free_head_out;
+  int32_t* ws;  // reorder_ws_ints()
+  int32_t R, max_pages, num_pages, num_free, page_shift;
+};
+size_t reorder_ws_ints(int32_t R, int32_t num_pages);
+hipError_t launch_kv_reorder(const ReorderArgs& a, hipStream_t s);
+
+constexpr int32_t kCopyMaxCaches = 64;  // of one launch: their pointers are its arguments
+struct CopyArgs {
+  void* pages[2 * kCopyMaxCaches];  // keys and values of every cache
+  const int32_t *src, *dst, *rows;  // rows NULL: whole pages
+  int32_t n, caches, num_pages, heads, page_shift, row_bytes;
+};
+hipError_t launch_kv_copy(const CopyArgs& a, hipStream_t s);
+
+struct BeamArgs {
+  const void* logits;
+  int64_t stride;
+  const float* scores;
+  const int32_t* done;  // or NULL
+  int32_t *parent, *token, *done_out;
+  float* score_out;
+  void* ws;  // beam_ws_bytes()
+  int32_t rows, beams, vocab, width, end_token, dtype;
+};
+size_t beam_ws_bytes(int32_t rows, int32_t vocab, int32_t width);
+hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s);
 
 }  // namespace sq
