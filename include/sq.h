@@ -653,6 +653,34 @@ sq_status sq_beam_select(const void* logits, int64_t stride, int32_t dtype, int3
                          int32_t* token, float* score_out, int32_t* done_out, void* workspace, size_t ws_bytes,
                          hipStream_t stream);
 
+/* Bytes of device workspace for sq_attn_shared (no initialization needed), at
+ * least 256; 0 for invalid arguments.  They serve every call with as many requests
+ * and groups or fewer and bounds as large or smaller.  Host-only. */
+size_t sq_attn_shared_workspace_bytes(int32_t num_requests, int32_t num_groups, int32_t q_heads, const sq_kv_cache* kv,
+                                      int32_t max_shared_len, int32_t max_own_len);
+
+/* sq_attn_paged (without a window) for requests that share their first tokens:
+ * group g is the requests group_start[g] .. group_start[g + 1] - 1, and their first
+ * p = shared_len[g] tokens (clamped to [0, max_shared_len]) are the same.  They are
+ * read once for the group, through the table row of its first request that has the
+ * most of them; tokens from p on are each request's own.  A request attends
+ * kv_len[r] tokens, also where that is less than p, and at most p + max_own_len;
+ * one of no group has p = 0.  Everything else (scores, what empty rows, NaN and
+ * infinities give, fp32 sums, cache rows that are not attended, the types and sizes)
+ * is as in sq_attn_paged; probabilities of the shared tokens enter their product
+ * with 16 (bf16) or 22 (f16) bits for 16-bit outputs, with all 24 for fp32 ones and
+ * for the requests' own tokens.
+ *   group_start  int32 [num_groups + 1], not falling, in [0, num_requests] (clamped;
+ *                requests of groups that overlap get unspecified results)
+ *   shared_len   int32 [num_groups]; both may be NULL with num_groups 0
+ * 0 <= num_groups <= 65535; max_shared_len and max_own_len each at most
+ * max_pages * page_size: they bound the work that is launched. */
+sq_status sq_attn_shared(const void* q, int64_t q_stride, int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv,
+                         const int32_t* table, int32_t max_pages, const int32_t* kv_len, const int32_t* group_start,
+                         const int32_t* shared_len, int32_t num_groups, int32_t max_shared_len, int32_t max_own_len,
+                         float scale, void* out, int32_t out_dtype, float* lse, void* workspace, size_t ws_bytes,
+                         hipStream_t stream);
+
 /* Bytes of device workspace for sq_kv_reorder with at most so many requests and
  * pages (no initialization needed), at least 256; 0 for invalid arguments.
  * Host-only. */

@@ -39,7 +39,8 @@ FLAGS = [
 
 SOURCES = ["sq_api.cpp", "quant_act.hip", "pack_weights.hip", "gemm_w4.hip", "gemm_skinny.hip", "unfused.hip",
            "mfma_probe.hip", "calib.hip", "noalloc.hip", "gelu.hip", "kv_plan.hip", "qk_norm_rope.hip",
-           "attn_paged.hip", "linear_w4a16.hip", "add_rmsnorm.hip", "beam_select.hip", "kv_reorder.hip", "kv_copy.hip"]
+           "attn_paged.hip", "linear_w4a16.hip", "add_rmsnorm.hip", "beam_select.hip", "kv_reorder.hip", "kv_copy.hip",
+           "attn_shared.hip"]
 
 
 _REMARK = re.compile(r"remark: Function Name: (\S+)|remark:\s+(ScratchSize \[bytes/lane\]|VGPRs Spill): (\d+)")

@@ -172,6 +172,9 @@ _SIGS = {
                             ctypes.POINTER(sq_act_params), _P, _P, _P]),
     "sq_beam_workspace_bytes": (_S, [_I, _I, _I, _I]),
     "sq_beam_select": (_I, [_P, _L, _I, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _S, _P]),
+    "sq_attn_shared_workspace_bytes": (_S, [_I, _I, _I, ctypes.POINTER(sq_kv_cache), _I, _I]),
+    "sq_attn_shared": (_I, [_P, _L, _I, _I, ctypes.POINTER(sq_kv_cache), _P, _I, _P, _P, _P, _I, _I, _I, ctypes.c_float,
+                            _P, _I, _P, _P, _S, _P]),
     "sq_kv_reorder_workspace_bytes": (_S, [_I, _I]),
     "sq_kv_reorder": (_I, [_P, _P, _I, _I, _I, _P, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
     "sq_kv_copy_pages": (_I, [ctypes.POINTER(sq_kv_cache), _I, _P, _P, _P, _I, _P]),
@@ -770,6 +773,33 @@ def sq_beam_select(logits: torch.Tensor, beams: int, scores: torch.Tensor, done:
                                 _ptr(token), _ptr(score_out), _ptr(done_out), wp, wb, _stream(stream)), "sq_beam_select")
 
 
+def sq_attn_shared_workspace_bytes(num_requests: int, num_groups: int, q_heads: int, kv: KVCache, max_shared_len: int,
+                                   max_own_len: int) -> int:
+    return int(lib().sq_attn_shared_workspace_bytes(num_requests, num_groups, q_heads, ctypes.byref(kv.struct()), max_shared_len,
+                                                    max_own_len))
+
+
+def sq_attn_shared(q: torch.Tensor, kv: KVCache, table: torch.Tensor, kv_len: torch.Tensor, group_start: torch.Tensor,
+                   shared_len: torch.Tensor, max_shared_len: int, max_own_len: int, scale: float, out: torch.Tensor,
+                   out_dtype: int, lse: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    """Attention of one query [R, q_heads, D] per request over the cache's pages table
+    [R, max_pages], where the requests group_start[g] .. group_start[g + 1] - 1 share their
+    first shared_len[g] tokens (include/sq.h)."""
+    c = kv.struct()
+    R, Hq, D = q.shape
+    qp, qs = _heads(q, kv.k.dtype, R, c.head_dim)
+    _typed(torch.int32, table, kv_len, group_start, shared_len)
+    _typed(torch.float32, lse)
+    if (out.shape != q.shape or out.dtype != OUT_DTYPES.get(out_dtype) or table.dim() != 2 or table.shape[0] != R
+            or kv_len.shape != (R,) or shared_len.dim() != 1 or group_start.shape != (shared_len.shape[0] + 1,)
+            or (lse is not None and lse.shape != (R, Hq))):
+        raise ValueError("sq_attn_shared: the tensors' sizes or types do not fit together")
+    wp, wb = _ws(workspace)
+    _check(lib().sq_attn_shared(qp, qs, R, Hq, ctypes.byref(c), _ptr(table), table.shape[1], _ptr(kv_len),
+                                _ptr(group_start), _ptr(shared_len), shared_len.shape[0], max_shared_len, max_own_len,
+                                scale, _ptr(out), out_dtype, _ptr(lse), wp, wb, _stream(stream)), "sq_attn_shared")
+
+
 def sq_kv_reorder_workspace_bytes(num_requests: int, num_pages: int) -> int:
     return int(lib().sq_kv_reorder_workspace_bytes(num_requests, num_pages))
 
@@ -814,6 +844,14 @@ def alloc_beam_workspace(num_rows: int, beams: int, vocab: int, width: int, devi
     if n == 0:
         raise ValueError("invalid sizes for a beam workspace")
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_attn_shared_workspace(num_requests: int, num_groups: int, q_heads: int, kv: KVCache, max_shared_len: int,
+                                max_own_len: int) -> torch.Tensor:
+    n = sq_attn_shared_workspace_bytes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len)
+    if n == 0:
+        raise ValueError("invalid sizes for an attention workspace")
+    return torch.empty(n, dtype=torch.uint8, device=kv.k.device)
 
 
 def alloc_reorder_workspace(num_requests: int, num_pages: int, device="cuda") -> torch.Tensor:

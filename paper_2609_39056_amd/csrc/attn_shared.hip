@@ -1,0 +1,487 @@
+// Attention of one new token per request where groups of requests share their
+// first tokens (sq_attn_shared).  Those are read once for a group instead of once
+// for each of its requests: the group's query rows (requests x query heads of a
+// key-value head) meet each tile of keys together.
+//
+// Three kernels: the prefix in chunks for tiles of a group's query rows, each
+// request's own tokens, and the join of both kinds of parts.  A part holds a
+// running maximum m (in units of log 2), a sum l and the weighted values.
+//
+// A wave takes 32 tokens at a time for Q tiles of 16 query rows, as in the paged
+// attention: scores as keys x queries, so that a lane has the probabilities that it
+// needs for the values, which it transposes in registers; nothing is passed
+// between lanes.  The waves of a workgroup take the tiles of a chunk in turn and
+// are joined through LDS.
+#include <type_traits>
+
+#include "attn_shared_split.h"
+#include "attn_tile.h"
+#include "token_internal.h"
+
+namespace sq {
+namespace {
+
+constexpr int kTile = kAttnTile, kQTile = kAttnQTile;
+constexpr int kMinPage = 8;
+constexpr int kWaves = 4;
+
+// The parts of the prefix and of the requests' own tokens, [row][chunk] of each
+// kind: D values, then maximum and sum; then the token ranges of the requests.
+struct Parts {
+  float *prefix, *mine;
+  float2 *prefix_stat, *mine_stat;
+  int2* range;  // own tokens [x, y)
+};
+__host__ __device__ inline Parts parts_of(const SharedArgs& a, const SharedSplit& sp) {
+  const size_t rows = static_cast<size_t>(a.R) * a.Hq;
+  Parts p;
+  p.prefix = static_cast<float*>(a.ws);
+  p.mine = p.prefix + rows * sp.count * a.D;
+  p.prefix_stat = reinterpret_cast<float2*>(p.mine + rows * sp.mine.count * a.D);
+  p.mine_stat = p.prefix_stat + rows * sp.count;
+  p.range = reinterpret_cast<int2*>(p.mine_stat + rows * sp.mine.count);
+  return p;
+}
+
+__device__ __forceinline__ int group_start(const SharedArgs& a, int g) { return min(max(a.group_start[g], 0), a.R); }
+__device__ __forceinline__ int64_t capacity(const SharedArgs& a) { return static_cast<int64_t>(a.max_pages) << a.page_shift; }
+__device__ __forceinline__ int shared_len(const SharedArgs& a, int g) {
+  return static_cast<int>(min(static_cast<int64_t>(min(max(a.shared_len[g], 0), a.max_shared)), capacity(a)));
+}
+__device__ __forceinline__ int kv_len(const SharedArgs& a, int r) {
+  return static_cast<int>(min(static_cast<int64_t>(max(a.kv_len[r], 0)), capacity(a)));
+}
+
+// The last group g with place(g) <= x, by all lanes of a wave (place does not fall).
+template <typename Place>
+__device__ int last_group(const SharedArgs& a, int64_t x, Place place) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  for (int step = a.groups > 4096 ? 4096 : a.groups > 64 ? 64 : 1;; step /= 64) {
+    const int64_t g = lo + static_cast<int64_t>(lane) * step;
+    const uint64_t before = __ballot(g < a.groups && place(static_cast<int>(g)) <= x);
+    lo += max(static_cast<int>(__popcll(before)) - 1, 0) * step;
+    if (step == 1) return lo;
+  }
+}
+
+// Q tiles of query rows against one chunk: the prefix of a group (OWN false) or a
+// request's own tokens; probabilities as NP 16-bit parts.
+template <bool F16, int D, int Q, int NP, bool OWN>
+__global__ __launch_bounds__(64 * kWaves, Q < 4 && D <= 128 ? 2 : 1) void shared_kernel(SharedArgs a, SharedSplit sp) {
+  constexpr int W = kWaves;
+  constexpr int KF = D / 32;  // fragments of a key row
+  constexpr int E = D / 16, E0 = E < 8 ? E : 8, E1 = E - E0;  // a lane's dimensions of a value row
+  constexpr int EW = E / 2;
+  constexpr bool kAhead = D < 256;
+  constexpr int kPages = (OWN ? kAttnWhole : static_cast<int>(kSharedMost)) / kMinPage + 2;
+  constexpr int kRows = Q * kQTile;
+  constexpr float kShift = F16 ? 11.0f : 0.0f;
+  constexpr float kSlack = F16 ? 4.0f : 8.0f;
+  __shared__ int32_t pages[kPages];
+  __shared__ float s_m[W][kQTile], s_l[W][kQTile], s_o[W][kQTile][D + 4];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int each = a.Hq / a.Hk;
+  const Parts parts = parts_of(a, sp);
+
+  // Query rows are numbered row0 ..: row i is head kvh * each + i % each of request
+  // req0 + i / each; there are `rows` of them here.
+  int kvh, split, req0, row0, rows, reader, first, stop, base, chunk;
+  if constexpr (OWN) {
+    const int r = blockIdx.y;
+    uint32_t wg = blockIdx.x;
+    const uint32_t qtiles = static_cast<uint32_t>((each + kRows - 1) / kRows);
+    kvh = static_cast<int>(wg % static_cast<uint32_t>(a.Hk));
+    wg /= static_cast<uint32_t>(a.Hk);
+    row0 = static_cast<int>(wg % qtiles) * kRows;
+    split = static_cast<int>(wg / qtiles);
+    const int group = last_group(a, r, [&](int i) { return static_cast<int64_t>(group_start(a, i)); });
+    const bool member = a.groups > 0 && group_start(a, group) <= r && r < group_start(a, group + 1);
+    const int p = member ? shared_len(a, group) : 0;
+    const int n = kv_len(a, r);
+    first = min(p, n);
+    stop = static_cast<int>(min(static_cast<int64_t>(n), static_cast<int64_t>(p) + a.max_own));
+    if (blockIdx.x == 0 && threadIdx.x == 0) parts.range[r] = make_int2(first, stop);
+    reader = req0 = r;
+    rows = min(each - row0, kRows);
+    base = first & ~(kTile - 1);
+    chunk = sp.mine.chunk;
+  } else {
+    // tiles of one (key-value head, chunk) stand 8 apart: on one XCD, whose cache
+    // then has the keys and values
+    const uint32_t id = blockIdx.x, slots = static_cast<uint32_t>(sp.slots);
+    const uint32_t pair = id / 8 / slots * 8 + id % 8, slot = id / 8 % slots;
+    if (pair >= static_cast<uint32_t>(a.Hk * sp.count)) return;
+    kvh = static_cast<int>(pair % static_cast<uint32_t>(a.Hk));
+    split = static_cast<int>(pair / static_cast<uint32_t>(a.Hk));
+    // group i has the slots from start * each / rows + i on, at least as many as it needs
+    auto place = [&](int i) { return static_cast<int64_t>(group_start(a, i)) * each / kRows + i; };
+    const int group = last_group(a, slot, place);
+    const int s0 = group_start(a, group), s1 = group_start(a, group + 1);
+    row0 = static_cast<int>(slot - place(group)) * kRows;
+    if (row0 < 0 || s1 <= s0 || row0 >= (s1 - s0) * each) return;
+    rows = min((s1 - s0) * each - row0, kRows);
+    req0 = s0;
+    chunk = sp.chunk;
+    // its tokens are read through the first request that has the most of them
+    const int p = shared_len(a, group);
+    if (split * static_cast<int64_t>(chunk) >= p) return;
+    reader = s0;
+    stop = 0;
+    for (int m = s0; m < s1 && stop < p; m += 64) {
+      int n = m + lane < s1 ? min(kv_len(a, m + lane), p) : 0;
+      int top = n;
+#pragma unroll
+      for (int o = 32; o >= 1; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+      if (top > stop) {
+        stop = top;
+        reader = m + __ffsll(static_cast<unsigned long long>(__ballot(n == top))) - 1;
+      }
+    }
+    first = base = 0;
+  }
+  const int64_t begin64 = base + static_cast<int64_t>(split) * chunk;
+  if (begin64 >= stop) return;
+  const int begin = static_cast<int>(begin64);
+  const int end = begin + min(stop - begin, chunk);
+  const int shift = a.page_shift, mask = (1 << shift) - 1;
+  const int page0 = begin >> shift, npages = ((end - 1) >> shift) - page0 + 1;
+  for (int i = threadIdx.x; i < npages; i += 64 * W) {
+    const int32_t p = a.table[static_cast<size_t>(reader) * a.max_pages + page0 + i];
+    pages[i] = p >= 0 && p < a.num_pages ? p : -1;
+  }
+
+  // queries: column c of tile y is row 16 y + c, the lane's values 32 j + 8 g ..
+  uint4 q[Q][KF];
+  int limit[Q];  // tokens of the rows' requests
+  int least = stop;
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+    const int i = kQTile * y + c, at = row0 + min(i, rows - 1);
+    const int req = req0 + at / each, head = kvh * each + at % each;
+    limit[y] = OWN ? stop : kv_len(a, req);
+    least = min(least, limit[y]);
+    const uint16_t* qrow = a.q + req * a.q_stride + static_cast<size_t>(head) * D + 8 * g;
+#pragma unroll
+    for (int j = 0; j < KF; ++j) {
+      q[y][j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
+      if (i >= rows) q[y][j] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  if constexpr (!OWN) {
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+  }
+  __syncthreads();
+
+  v4f o[Q][E];
+  float m[Q], l[Q];
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[y][e] = v4f{0, 0, 0, 0};
+    m[y] = kLowest;
+    l[y] = 0.0f;
+  }
+  const float scale = a.scale * kLog2e;
+
+  auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
+  auto row_of = [&](int page, int tok) {
+    return ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + (tok & mask);
+  };
+  // a tile's keys: tokens b + 16 i + c, the lane's values 32 j + 8 g ..; its
+  // values: tokens b + 16 i + 4 g + x, the lane's dimensions.  Tokens outside
+  // [first, end) are not loaded: their lanes repeat the nearest row inside.
+  const int tiles = (end - begin + kTile - 1) / kTile;
+  uint4 k[2][KF];
+  uint32_t v[8][EW];
+  int kp[2], vp[2];
+  auto inside = [&](int b) { return b >= first && b + kTile <= end; };
+  auto load_v_row = [&](const uint16_t* p, uint32_t* w) {
+    load_words<E0 / 2, OWN>(p + E0 * c, w);
+    if constexpr (E1 > 0) load_words<E1 / 2, OWN>(p + 16 * E0 + E1 * c, w + E0 / 2);
+  };
+  auto load_k = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int tok = max(first, min(b + 16 * i + c, end - 1));
+      kp[i] = page_of(tok);
+      const uint16_t* p = a.k + row_of(kp[i], tok) * D + 8 * g;
+#pragma unroll
+      for (int j = 0; j < KF; ++j) k[i][j] = load16<OWN>(p + 32 * j);
+    }
+  };
+  auto load_v = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int tok = b + 16 * i + 4 * g, tc = max(first, min(tok, end - 1));
+      vp[i] = page_of(tc);
+      const uint16_t* p = a.v + row_of(vp[i], tc) * D;
+      if (inside(b)) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) load_v_row(p + x * D, v[4 * i + x]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) load_v_row(p + max(0, min(tok + x, end - 1) - tc) * D, v[4 * i + x]);
+      }
+    }
+  };
+  if (kAhead && wave < tiles) {
+    load_k(begin + wave * kTile);
+    load_v(begin + wave * kTile);
+  }
+  for (int t = wave; t < tiles; t += W) {
+    const int b = begin + t * kTile;
+    if (!kAhead) {
+      load_k(b);
+      load_v(b);
+    }
+    float f[Q][8];
+#pragma unroll
+    for (int y = 0; y < Q; ++y) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        v4f s = v4f{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < KF; ++j) s = mfma<F16>(k[i][j], q[y][j], s);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[x] * scale;
+      }
+    }
+    const bool whole_tile = inside(b) && b + kTile <= least && __all(kp[0] >= 0 && kp[1] >= 0);
+    if (kAhead && t + W < tiles) load_k(b + W * kTile);
+    if (!whole_tile) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
+        const bool live = (tok >= first) & (tok < end) & (vp[i / 4] >= 0);
+#pragma unroll
+        for (int y = 0; y < Q; ++y) f[y][i] = (live & (tok < limit[y])) ? f[y][i] : -INFINITY;
+#pragma unroll
+        for (int w = 0; w < EW; ++w) v[i][w] = live ? v[i][w] : 0;
+      }
+    }
+    uint32_t p[Q][NP][4];
+#pragma unroll
+    for (int y = 0; y < Q; ++y) {
+      float top = f[y][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, f[y][i]);
+      if (__any(top > m[y] + kSlack)) {
+        const float mn = fmaxf(m[y], quad_max(top));
+        const float al = __builtin_amdgcn_exp2f(m[y] - mn);
+        m[y] = mn;
+        l[y] *= al;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[y][e] *= al;
+      }
+      const float from = m[y] - kShift;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        float x0 = __builtin_amdgcn_exp2f(f[y][i] - from), x1 = __builtin_amdgcn_exp2f(f[y][i + 1] - from);
+        l[y] += x0 + x1;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          p[y][u][i / 2] = to_half2<F16>(x0, x1);
+          x0 -= half_lo<F16>(p[y][u][i / 2]);
+          x1 -= half_hi<F16>(p[y][u][i / 2]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      uint4 vt;
+      const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+      vt.x = __builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel);
+      vt.y = __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel);
+      vt.z = __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel);
+      vt.w = __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel);
+#pragma unroll
+      for (int y = 0; y < Q; ++y)
+#pragma unroll
+        for (int u = 0; u < NP; ++u)
+          o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
+    }
+    if (kAhead && t + W < tiles) load_v(b + W * kTile);
+  }
+
+  // the waves' parts, a tile of rows at a time: column c, and the dimensions that lane 4 g + x loaded
+  float* out = OWN ? parts.mine : parts.prefix;
+  float2* stat = OWN ? parts.mine_stat : parts.prefix_stat;
+  const int count = OWN ? sp.mine.count : sp.count;
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+    if (kQTile * y >= rows) break;
+    const float ls = quad_sum(l[y]);
+    if (y > 0) __syncthreads();
+    if (g == 0) {
+      s_m[wave][c] = m[y] - kShift;
+      s_l[wave][c] = ls;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        s_o[wave][c][e < E0 ? E0 * (4 * g + x) + e : 16 * E0 + E1 * (4 * g + x) + e - E0] = o[y][e][x];
+    __syncthreads();
+    const int here = min(rows - kQTile * y, kQTile);
+    for (int i = threadIdx.x; i < here * (D / 4); i += 64 * W) {
+      const int qh = i / (D / 4), d4 = i % (D / 4);
+      float M = s_m[0][qh], L = 0.0f;
+#pragma unroll
+      for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][qh]);
+      float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const float al = __builtin_amdgcn_exp2f(s_m[w][qh] - M);
+        L = __builtin_fmaf(s_l[w][qh], al, L);
+        add_scaled(sum, *reinterpret_cast<const float4*>(&s_o[w][qh][4 * d4]), al);
+      }
+      const int at = row0 + kQTile * y + qh, req = req0 + at / each, head = kvh * each + at % each;
+      // Parts of a probability may be 0 or negative, and 0 meets values of tokens that a
+      // shorter request does not attend: where that leaves NaN the formula is followed token by token.
+      if (is_nan(sum.x + sum.y + sum.z + sum.w) && !is_nan(L)) {
+        sum = make_float4(0, 0, 0, 0);
+        const uint4* qr = reinterpret_cast<const uint4*>(a.q + req * a.q_stride + static_cast<size_t>(head) * D);
+        const int last = OWN ? end : min(end, kv_len(a, req));
+        for (int tok = max(first, begin); tok < last; ++tok) {
+          const int page = page_of(tok);
+          if (page < 0) continue;
+          const size_t row = row_of(page, tok) * D;
+          const uint4* kr = reinterpret_cast<const uint4*>(a.k + row);
+          float dot = 0.0f;
+#pragma unroll 1  // its registers are the kernel's
+          for (int j = 0; j < D / 8; ++j) {
+            float u[8], w8[8];
+            widen8<F16>(qr[j], u);
+            widen8<F16>(kr[j], w8);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) dot = __builtin_fmaf(u[x], w8[x], dot);
+          }
+          const uint2 raw = *reinterpret_cast<const uint2*>(a.v + row + 4 * d4);
+          add_scaled(sum, make_float4(half_lo<F16>(raw.x), half_hi<F16>(raw.x), half_lo<F16>(raw.y), half_hi<F16>(raw.y)),
+                     __builtin_amdgcn_exp2f(dot * scale - M));
+        }
+      }
+      const size_t part = (static_cast<size_t>(req) * a.Hq + head) * count + split;
+      reinterpret_cast<float4*>(out)[part * (D / 4) + d4] = sum;
+      if (d4 == 0) stat[part] = make_float2(M, L);
+    }
+  }
+}
+
+// Joins the parts of a query head: a thread takes four dimensions.
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a, SharedSplit sp) {
+  const int D4 = a.D / 4;
+  const size_t i = flat_wg() * 256 + threadIdx.x, row = i / D4;
+  if (row >= static_cast<size_t>(a.R) * a.Hq) return;
+  const int d4 = static_cast<int>(i % D4);
+  const Parts parts = parts_of(a, sp);
+  const int2 range = parts.range[row / a.Hq];
+  const int np = (range.x + sp.chunk - 1) / sp.chunk;
+  const int from = range.x & ~(kTile - 1);
+  const int nm = range.y > range.x ? (range.y - from + sp.mine.chunk - 1) / sp.mine.chunk : 0;
+  float M = kLowest, L = 0.0f;
+  float4 v = make_float4(0, 0, 0, 0);
+  auto join = [&](const float* part, const float2* stat, int count, int n) {
+    const float4* po = reinterpret_cast<const float4*>(part) + row * count * D4 + d4;
+    const float2* ps = stat + row * count;
+    constexpr int kTogether = 8;  // parts whose loads are in flight together
+    for (int s0 = 0; s0 < n; s0 += kTogether) {
+      float2 ml[kTogether];
+      float4 o[kTogether];
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        const int s = min(s0 + u, n - 1);
+        ml[u] = ps[s];
+        o[u] = po[static_cast<size_t>(s) * D4];
+        if (s0 + u >= n) ml[u] = make_float2(kLowest, 0.0f);
+      }
+      float mn = M;
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) mn = fmaxf(mn, ml[u].x);
+      const float was = __builtin_amdgcn_exp2f(M - mn);
+      M = mn;
+      L *= was;
+      v = make_float4(v.x * was, v.y * was, v.z * was, v.w * was);
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        if (s0 + u >= n) break;
+        const float al = __builtin_amdgcn_exp2f(ml[u].x - mn);
+        L = __builtin_fmaf(ml[u].y, al, L);
+        add_scaled(v, o[u], al);
+      }
+    }
+  };
+  join(parts.prefix, parts.prefix_stat, sp.count, np);
+  join(parts.mine, parts.mine_stat, sp.mine.count, nm);
+  // an empty sum gives 0; a NaN one (of a NaN score, or one of +infinity) goes into both
+  const bool empty = L == 0.0f;
+  const float inv = empty ? 0.0f : 1.0f / L;
+  store_out4(a.out, row * D4 + d4, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv), a.out_dtype);
+  if (d4 == 0 && a.lse != nullptr) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
+}
+
+template <bool F16, int D, int Q, int NP>
+void launch_prefix(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
+  const unsigned pairs = static_cast<unsigned>((a.Hk * sp.count + 7) / 8 * 8);
+  shared_kernel<F16, D, Q, NP, false><<<pairs * static_cast<unsigned>(sp.slots), 64 * kWaves, 0, s>>>(a, sp);
+}
+
+template <bool F16, int D>
+void launch_dim(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
+  const bool fine = a.out_dtype == SQ_OUT_F32;
+  auto prefix = [&](auto tiles) {
+    constexpr int Q = decltype(tiles)::value;
+    fine ? launch_prefix<F16, D, Q, 3>(a, sp, s) : launch_prefix<F16, D, Q, 2>(a, sp, s);
+  };
+  if (sp.count > 0 && a.groups > 0) {
+    if (sp.q == 1) {
+      prefix(std::integral_constant<int, 1>{});
+    } else if (sp.q == 2) {
+      prefix(std::integral_constant<int, 2>{});
+    } else if constexpr (D <= 128) {
+      prefix(std::integral_constant<int, kSharedTiles>{});
+    }
+  }
+  const int each = a.Hq / a.Hk;
+  const dim3 grid(a.Hk * ((each + kQTile - 1) / kQTile) * sp.mine.count, static_cast<unsigned>(a.R));
+  shared_kernel<F16, D, 1, 3, true><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+}
+
+template <bool F16>
+void launch_type(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
+  switch (a.D) {
+    case 64: return launch_dim<F16, 64>(a, sp, s);
+    case 96: return launch_dim<F16, 96>(a, sp, s);
+    case 128: return launch_dim<F16, 128>(a, sp, s);
+    case 192: return launch_dim<F16, 192>(a, sp, s);
+    default: return launch_dim<F16, 256>(a, sp, s);
+  }
+}
+
+}  // namespace
+
+size_t attn_shared_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t max_shared, int32_t max_own) {
+  return shared_ws_bytes(R, Hq, Hk, D, max_shared, max_own);
+}
+
+hipError_t launch_attn_shared(const SharedArgs& a, bool f16, hipStream_t s) {
+  const SharedSplit sp = shared_split(a.R, a.groups, a.Hq, a.Hk, a.D, a.max_shared, a.max_own);
+  const Parts p = parts_of(a, sp);
+  const size_t used = reinterpret_cast<const char*>(p.range + a.R) - static_cast<const char*>(a.ws);
+  if (used > a.ws_bytes) return hipErrorInvalidValue;
+  const int64_t wgs = static_cast<int64_t>(a.Hk * sp.count + 7) / 8 * 8 * sp.slots;
+  const int64_t mine = static_cast<int64_t>(a.Hk) * ((a.Hq / a.Hk + kQTile - 1) / kQTile) * sp.mine.count;
+  if (wgs >= (1 << 24) || mine >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
+  f16 ? launch_type<true>(a, sp, s) : launch_type<false>(a, sp, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const size_t n = static_cast<size_t>(a.R) * a.Hq * (a.D / 4);
+  shared_join_kernel<<<wg_grid((n + 255) / 256), 256, 0, s>>>(a, sp);
+  return hipGetLastError();
+}
+
+}  // namespace sq

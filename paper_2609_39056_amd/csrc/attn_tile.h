@@ -36,15 +36,19 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
+// Loads of a row's pieces: past the caches where a row is read once (STREAM).
+template <bool STREAM = true>
 __device__ __forceinline__ uint4 load16(const uint16_t* p) {
   typedef unsigned int vec __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const vec*>(p)));
+  const vec* q = reinterpret_cast<const vec*>(p);
+  return __builtin_bit_cast(uint4, STREAM ? __builtin_nontemporal_load(q) : *q);
 }
 // N dwords from a 4-byte boundary.
-template <int N>
+template <int N, bool STREAM = true>
 __device__ __forceinline__ void load_words(const uint16_t* p, uint32_t* w) {
   typedef unsigned int vec __attribute__((ext_vector_type(N), aligned(4)));
-  const vec r = __builtin_nontemporal_load(reinterpret_cast<const vec*>(p));
+  const vec* q = reinterpret_cast<const vec*>(p);
+  const vec r = STREAM ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
   for (int i = 0; i < N; ++i) w[i] = r[i];
 }

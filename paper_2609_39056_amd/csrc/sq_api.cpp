@@ -383,6 +383,10 @@ bool valid_attn_sizes(int32_t R, int32_t Hq, const sq_kv_cache* kv, int32_t max_
   return R >= 0 && R <= kMaxRequests && Hq >= 1 && Hq <= kMaxQHeads && Hq % kv->num_heads == 0 && max_kv_len >= 0;
 }
 
+bool valid_shared_sizes(int32_t R, int32_t groups, int32_t Hq, const sq_kv_cache* kv, int32_t max_shared, int32_t max_own) {
+  return valid_attn_sizes(R, Hq, kv, max_shared) && max_own >= 0 && groups >= 0 && groups <= kMaxRequests;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1092,6 +1096,63 @@ sq_status sq_beam_select(const void* logits, int64_t stride, int32_t dtype, int3
   BeamArgs a{logits, stride, scores, done, parent, token, done_out, score_out, workspace, num_rows, beams, vocab, width,
              end_token, dtype};
   return hip_status(launch_beam_select(a, stream));
+}
+
+size_t sq_attn_shared_workspace_bytes(int32_t num_requests, int32_t num_groups, int32_t q_heads, const sq_kv_cache* kv,
+                                      int32_t max_shared_len, int32_t max_own_len) {
+  if (check_cache(kv) != SQ_OK || !valid_shared_sizes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len))
+    return 0;
+  return std::max(kAlign, round_up(attn_shared_bytes(num_requests, q_heads, kv->num_heads, kv->head_dim, max_shared_len,
+                                                     max_own_len)));
+}
+
+sq_status sq_attn_shared(const void* q, int64_t q_stride, int32_t num_requests, int32_t q_heads, const sq_kv_cache* kv,
+                         const int32_t* table, int32_t max_pages, const int32_t* kv_len, const int32_t* group_start,
+                         const int32_t* shared_len, int32_t num_groups, int32_t max_shared_len, int32_t max_own_len,
+                         float scale, void* out, int32_t out_dtype, float* lse, void* workspace, size_t ws_bytes,
+                         hipStream_t stream) {
+  const sq_status st = check_cache(kv);
+  if (st != SQ_OK) return st;
+  if (!valid_out(out_dtype) || !std::isfinite(scale)) return SQ_ERR_UNSUPPORTED;
+  const int64_t most = static_cast<int64_t>(max_pages) * kv->page_size;
+  if (!valid_shared_sizes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len) || max_pages < 1 || most >= kIndexEnd || max_shared_len > most || max_own_len > most)
+    return SQ_ERR_SHAPE;
+  if (num_requests == 0) return SQ_OK;
+  if (q == nullptr || table == nullptr || kv_len == nullptr || out == nullptr || workspace == nullptr ||
+      (num_groups > 0 && (group_start == nullptr || shared_len == nullptr)))
+    return SQ_ERR_NULL;
+  if (!valid_stride(q_stride, q_heads, kv->head_dim)) return SQ_ERR_SHAPE;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(table, 4) || !aligned(kv_len, 4) ||
+      !aligned(group_start, 4) || !aligned(shared_len, 4) || !aligned(lse, 4))
+    return SQ_ERR_ALIGN;
+  if (ws_bytes < sq_attn_shared_workspace_bytes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len))
+    return SQ_ERR_WORKSPACE;
+  SharedArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(kv->k);
+  a.v = static_cast<const uint16_t*>(kv->v);
+  a.q_stride = q_stride;
+  a.table = table;
+  a.kv_len = kv_len;
+  a.group_start = group_start;
+  a.shared_len = shared_len;
+  a.out = out;
+  a.lse = lse;
+  a.ws = workspace;
+  a.ws_bytes = ws_bytes;
+  a.R = num_requests;
+  a.groups = num_groups;
+  a.Hq = q_heads;
+  a.Hk = kv->num_heads;
+  a.D = kv->head_dim;
+  a.max_pages = max_pages;
+  a.num_pages = kv->num_pages;
+  a.page_shift = log2_of(kv->page_size);
+  a.max_shared = max_shared_len;
+  a.max_own = max_own_len;
+  a.out_dtype = out_dtype;
+  a.scale = scale;
+  return hip_status(launch_attn_shared(a, kv->dtype == SQ_OUT_F16, stream));
 }
 
 size_t sq_kv_reorder_workspace_bytes(int32_t num_requests, int32_t num_pages) {

@@ -85,6 +85,20 @@ struct CopyArgs {
 };
 hipError_t launch_kv_copy(const CopyArgs& a, hipStream_t s);
 
+struct SharedArgs {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride;
+  const int32_t *table, *kv_len, *group_start, *shared_len;
+  void* out;
+  float* lse;  // or NULL
+  void* ws;    // attn_shared_bytes()
+  size_t ws_bytes;
+  int32_t R, groups, Hq, Hk, D, max_pages, num_pages, page_shift, max_shared, max_own, out_dtype;
+  float scale;
+};
+size_t attn_shared_bytes(int32_t R, int32_t Hq, int32_t Hk, int32_t D, int32_t max_shared, int32_t max_own);
+hipError_t launch_attn_shared(const SharedArgs& a, bool f16, hipStream_t s);
+
 struct BeamArgs {
   const void* logits;
   int64_t stride;

@@ -1,0 +1,87 @@
+"""How attention over shared prefixes is split (csrc/attn_shared_split.h) and its
+workspace, asked on the host: what has to hold for every size."""
+import random
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2609_39056_amd import _build
+
+SRC = """
+#include "attn_shared_split.h"
+#include <stdio.h>
+using namespace sq;
+int main() {
+  int R, groups, Hq, Hk, D, shared, own, R2, shared2, own2;
+  while (scanf("%d %d %d %d %d %d %d %d %d %d", &R, &groups, &Hq, &Hk, &D, &shared, &own, &R2, &shared2, &own2) == 10) {
+    const SharedSplit s = shared_split(R, groups, Hq, Hk, D, shared, own);
+    const size_t used = (size_t)R * Hq * ((size_t)s.count + s.mine.count) * (D + 2) * 4 + (size_t)R * 8;
+    printf("%d %d %d %d %d %d %zu %zu %zu\\n", s.q, s.slots, s.chunk, s.count, s.mine.chunk, s.mine.count, used,
+           shared_ws_bytes(R, Hq, Hk, D, shared, own), shared_ws_bytes(R2, Hq, Hk, D, shared2, own2));
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def split(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("clang++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    d = tmp_path_factory.mktemp("shared")
+    (d / "split.cpp").write_text(SRC)
+    subprocess.run([cxx, "-std=c++17", "-O1", f"-I{_build.CSRC}", str(d / "split.cpp"), "-o", str(d / "split")], check=True)
+
+    def ask(rows):
+        text = "\n".join(" ".join(map(str, r)) for r in rows) + "\n"
+        out = subprocess.run([str(d / "split")], input=text, capture_output=True, text=True, check=True).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+
+    return ask
+
+
+HEADS = [(16, 16, 128), (40, 8, 128), (8, 1, 256), (32, 1, 128), (20, 20, 96), (14, 2, 64), (12, 12, 192), (1024, 256, 64), (1, 1, 64)]
+
+
+def cases():
+    rng = random.Random(2)
+    edges = [0, 1, 31, 32, 33, 127, 128, 129, 1249, 1250, 8191, 8192, 8193, 131072, 2 ** 31 - 1]
+    for heads in HEADS:
+        for shared in edges:
+            for own in (0, 1, 353, 354, 1249, 1250, 2 ** 31 - 1):
+                for R, groups in ((1, 0), (1, 1), (4, 1), (64, 1), (64, 16), (65535, 65535), (7, 65535)):
+                    yield (R, groups, *heads, shared, own, R, shared, own)
+    for _ in range(20000):
+        R, shared, own = int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 24)) - 1, int(2 ** rng.uniform(0, 20)) - 1
+        yield (R, int(R * rng.random() ** 3), *rng.choice(HEADS), shared, own, R + rng.choice([0, 1, int(2 ** rng.uniform(0, 14))]),
+               shared + rng.choice([0, 1, int(2 ** rng.uniform(0, 24))]), own + rng.choice([0, 1, int(2 ** rng.uniform(0, 20))]))
+
+
+def test_chunks_cover_the_prefix_and_a_larger_workspace_holds_the_parts(split):
+    asked = list(cases())
+    for row, (q, slots, chunk, count, mine, mines, used, need, larger) in zip(asked, split(asked)):
+        R, groups, Hq, Hk, D, shared, own = row[:7]
+        assert q in (1, 2, 4) and (D <= 128 or q <= 2), row
+        assert chunk % 32 == 0 and 128 <= chunk <= 8192 and chunk * count >= shared > chunk * (count - 1), row
+        assert mine % 32 == 0 and mine <= 1280 and mine * mines >= own + 31, row  # from a multiple of 32 on
+        assert used <= need <= larger, row
+
+
+def test_every_group_has_the_slots_that_its_rows_need(split):
+    rng = random.Random(4)
+    for Hq, Hk, D in HEADS:
+        for trial in range(60):
+            groups = int(2 ** rng.uniform(0, 10))
+            sizes = [rng.choice([0, 0, 1, 1, 2, rng.randint(0, 9), rng.randint(0, 200)]) for _ in range(groups)]
+            before, behind = rng.choice([0, 3]), rng.choice([0, 5])
+            R = sum(sizes) + before + behind
+            if not 0 < R < 65536:
+                continue
+            (q, slots, *_), = split([(R, groups, Hq, Hk, D, 1000, 10, R, 1000, 10)])
+            rows, each, at = 16 * q, Hq // Hk, before
+            for g, n in enumerate(sizes):
+                first, then = at * each // rows + g, (at + n) * each // rows + g + 1
+                assert -(-n * each // rows) <= then - first
+                assert first + -(-n * each // rows) <= slots
+                at += n

@@ -97,6 +97,41 @@ def test_reorder_workspace(L):  # noqa: F811
     assert n(1, 1) == 256 and n(8192, 1 << 20) >= 4 << 20 and n(0, 5) == 0 and n(8193, 5) == 0 and n(4, 0) == 0
 
 
+def shared(L, kv=None, no_cache=False, **kw):  # noqa: F811
+    d = dict(q=A, qs=2048, R=3, Hq=16, table=A, max_pages=8, kv_len=A, start=A, shared=A, groups=1, most=128, own=128, scale=0.1, out=A,
+             out_dtype=B.SQ_OUT_BF16, lse=None, ws=A, nbytes=1 << 30)
+    d.update(kw)
+    c = None if no_cache else ctypes.byref(cache(**(kv or {})))
+    return L.sq_attn_shared(d["q"], d["qs"], d["R"], d["Hq"], c, d["table"], d["max_pages"], d["kv_len"], d["start"], d["shared"],
+                            d["groups"], d["most"], d["own"], d["scale"], d["out"], d["out_dtype"], d["lse"], d["ws"], d["nbytes"],
+                            None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(no_cache=True), NULL), (dict(q=None), NULL), (dict(table=None), NULL), (dict(kv_len=None), NULL),
+    (dict(start=None), NULL), (dict(shared=None), NULL), (dict(out=None), NULL), (dict(ws=None), NULL), (dict(out_dtype=3), UNSUP),
+    (dict(scale=NAN), UNSUP), (dict(scale=INF), UNSUP), (dict(R=-1), SHAPE), (dict(R=65536), SHAPE), (dict(Hq=0), SHAPE),
+    (dict(Hq=15), SHAPE), (dict(Hq=1026), SHAPE), (dict(groups=-1), SHAPE), (dict(groups=65536), SHAPE), (dict(most=-1), SHAPE),
+    (dict(most=129), SHAPE), (dict(own=-1), SHAPE), (dict(own=129), SHAPE), (dict(max_pages=0), SHAPE),
+    (dict(max_pages=1 << 27), SHAPE), (dict(qs=2040), SHAPE), (dict(qs=2049), SHAPE), (dict(q=A + 8), ALIGN), (dict(out=A + 8), ALIGN),
+    (dict(ws=A + 8), ALIGN), (dict(table=A + 2), ALIGN), (dict(kv_len=A + 2), ALIGN), (dict(start=A + 2), ALIGN),
+    (dict(shared=A + 2), ALIGN), (dict(lse=A + 2), ALIGN), (dict(nbytes=255), WS), (dict(R=0), OK), (dict(R=0, q=None, ws=None), OK),
+] + [(dict(kv=kv), code) for kv, code in CACHE_CASES])
+def test_shared_rejects(L, kw, code):  # noqa: F811
+    assert shared(L, **kw) == code
+
+
+def test_shared_workspace(L):  # noqa: F811
+    def n(R, groups, Hq, most, own, **kw):
+        return L.sq_attn_shared_workspace_bytes(R, groups, Hq, ctypes.byref(cache(**kw)), most, own)
+
+    for args in ((0, 0, 16, 0, 0), (1, 1, 16, 0, 1), (64, 1, 16, 8192, 500), (2, 65535, 32, 131072, 131072)):
+        assert n(*args) >= 256 and n(*args) % 256 == 0
+    assert n(1, 1, 15, 100, 100) == 0 and n(-1, 1, 16, 100, 100) == 0 and n(1, -1, 16, 1, 1) == 0 and n(1, 1, 16, -1, 1) == 0
+    assert n(1, 1, 16, 1, -1) == 0 and n(1, 1, 16, 1, 1, page_size=3) == 0
+    assert L.sq_attn_shared_workspace_bytes(1, 1, 16, None, 100, 100) == 0
+
+
 def copy(L, caches=None, n_caches=None, null=False, **kw):  # noqa: F811
     d = dict(src=A, dst=A + 64, rows=None, n=3)
     d.update(kw)
@@ -134,6 +169,8 @@ def test_binding_refuses_host_tensors_sizes_and_types(L):  # noqa: F811
     with pytest.raises(ValueError, match="device tensors"):
         B.sq_kv_reorder(i, i, 16, 9, i, None, t, t, i, i, i, i, i, i)
     k = torch.zeros((2, 1, 8, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="device tensors"):
+        B.alloc_attn_shared_workspace(1, 1, 2, B.KVCache(k, k), 8, 8)
     with pytest.raises(ValueError, match="sizes"):
         B.sq_kv_copy_pages([], i, i[:1], None)
     with pytest.raises(ValueError, match="device tensors"):
