@@ -203,7 +203,7 @@ def _load_call():
         loader.exec_module(mod)
         if mod.built_for != _build.built_for():
             raise ImportError(f"built for {mod.built_for}, this is {_build.built_for()}")
-        if not hasattr(mod, "setup_token"):
+        if not hasattr(mod, "attn_shared"):
             raise ImportError("built from an older source")
     except ImportError as e:
         warnings.warn(f"{CALL_PATH}: {e}; arguments are marshalled with ctypes "
@@ -730,6 +730,11 @@ def sq_add_rmsnorm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: Op
     """h = x + residual [M, K] into sum_out, its root-mean-square norm into y (of
     out_dtype) and / or, with act, the 8-bit codes qx and row scales of a quantized
     linear (include/sq.h).  x, residual and sum_out may be views with contiguous rows."""
+    L = _lib or lib()
+    st = _call.norm(L.sq_address["sq_add_rmsnorm"], x, residual, weight, eps, sum_out, y, out_dtype, act, qx,
+                    act_scale, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_add_rmsnorm")
     M, K = x.shape
     xp, xs, xd = _rows(x, M, K)
     rp, rs, rd = _rows(residual, M, K)
@@ -758,6 +763,11 @@ def sq_beam_select(logits: torch.Tensor, beams: int, scores: torch.Tensor, done:
     """The width best continuations of every group of `beams` rows of logits [R, vocab]
     (rows may be a view's) into parent, token, score_out and done_out [R / beams, width]
     (include/sq.h)."""
+    L = _lib or lib()
+    st = _call.beams(L.sq_address["sq_beam_select"], logits, beams, scores, done, end_token, parent, token, score_out,
+                     done_out, workspace, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_beam_select")
     R, V = logits.shape
     xp, xs, xd = _rows(logits, R, V)
     _typed(torch.int32, done, parent, token, done_out)
@@ -785,6 +795,11 @@ def sq_attn_shared(q: torch.Tensor, kv: KVCache, table: torch.Tensor, kv_len: to
     """Attention of one query [R, q_heads, D] per request over the cache's pages table
     [R, max_pages], where the requests group_start[g] .. group_start[g + 1] - 1 share their
     first shared_len[g] tokens (include/sq.h)."""
+    L = _lib or lib()
+    st = _call.attn_shared(L.sq_address["sq_attn_shared"], q, kv, table, kv_len, group_start, shared_len, max_shared_len,
+                           max_own_len, scale, out, out_dtype, lse, workspace, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_attn_shared")
     c = kv.struct()
     R, Hq, D = q.shape
     qp, qs = _heads(q, kv.k.dtype, R, c.head_dim)
@@ -810,6 +825,11 @@ def sq_kv_reorder(parent: torch.Tensor, kv_len: torch.Tensor, page_size: int, nu
                   free_head_out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """Tables [R, max_pages] whose row r goes on from row parent[r], pages that come free,
     and the copies that sq_kv_copy_pages has to make (include/sq.h); every tensor int32."""
+    L = _lib or lib()
+    st = _call.reorder(L.sq_address["sq_kv_reorder"], parent, kv_len, page_size, num_pages, free_pages, free_head, table,
+                       table_out, kv_len_out, copy_src, copy_dst, copy_rows, free_head_out, workspace, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_kv_reorder")
     _typed(torch.int32, parent, kv_len, free_pages, free_head, table, table_out, kv_len_out, copy_src, copy_dst, copy_rows,
            free_head_out)
     if table.dim() != 2:
@@ -830,6 +850,10 @@ def sq_kv_copy_pages(caches: Sequence[KVCache], src: torch.Tensor, dst: torch.Te
                      stream=None) -> None:
     """The first rows[i] tokens of page src[i] to page dst[i] in every cache of the
     sequence (include/sq.h); src, dst and rows int32 [n], rows None: whole pages."""
+    L = _lib or lib()
+    st = _call.copy(L.sq_address["sq_kv_copy_pages"], caches, src, dst, rows, stream)
+    if st is not NotImplemented:
+        return _check(st, "sq_kv_copy_pages")
     _typed(torch.int32, src, dst, rows)
     if src.dim() != 1 or dst.shape != src.shape or (rows is not None and rows.shape != src.shape):
         raise ValueError("sq_kv_copy_pages: the tensors' sizes do not fit together")

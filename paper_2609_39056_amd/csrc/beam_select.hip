@@ -3,13 +3,16 @@
 //     total(b, t) = score[b] + x[b][t] - log sum_u exp(x[b][u])
 // and the `width` pairs (b, t) with the largest totals, in order.
 //
-// One pass over the logits.  A workgroup takes 4096 tokens of a row in
-// registers and leaves its maximum, its sum of exponentials and its `width`
-// best tokens, found by their keys: the logit's bits in the order of its value
-// above the inverted token number, unique whole numbers whose order is that of
-// the definition within a row.  A second kernel joins the chunks of each row of a
-// group and its rows.  Totals are fp64: beams of one prompt lie next to each
-// other.
+// One pass over the logits.  A workgroup takes a chunk of a row in registers and
+// leaves its maximum, its sum of exponentials and its `width` best tokens: the
+// width-th largest of 64 groups' maxima bounds them from below, the few values
+// that reach it are listed and ordered by their keys, the logit's bits in the
+// order of its value above the inverted token number: unique whole numbers whose
+// order is that of the definition within a row.  A second kernel joins the chunks
+// of each row of a group, in the same way, and the rows.  Totals are fp64: beams
+// of one prompt lie next to each other.
+#include <algorithm>
+
 #include "half_types.h"
 #include "token_internal.h"
 
@@ -19,10 +22,8 @@ namespace {
 typedef unsigned long long Key;  // 0: none
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kEach = 16;                  // values of a thread
-constexpr int kChunk = kThreads * kEach;   // tokens of a workgroup
 constexpr int kMaxWidth = 64;
-constexpr int kGroupOf = kWaves * kEach;   // values behind a maximum that the threshold is taken from
+constexpr int kList = 1024;  // values that a workgroup orders; more only where very many are equal
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Of one chunk of a row.
@@ -32,12 +33,13 @@ struct Stat {
   int32_t unused;
 };
 
-__host__ __device__ constexpr int chunks_of(int vocab) { return (vocab + kChunk - 1) / kChunk; }
-
+// Bits whose order is that of the values (-0 counts as 0).
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t u = __float_as_uint(v + 0.0f);
+  return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
 __device__ __forceinline__ Key key_of(float v, uint32_t token) {
-  const uint32_t u = __float_as_uint(v + 0.0f);  // -0 counts as 0
-  const uint32_t o = u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-  return (static_cast<Key>(o) << 32) | (0xFFFFFFFFu - token);
+  return (static_cast<Key>(order_of(v)) << 32) | (0xFFFFFFFFu - token);
 }
 __device__ __forceinline__ uint32_t token_of(Key k) { return 0xFFFFFFFFu - static_cast<uint32_t>(k); }
 __device__ __forceinline__ float value_of(Key k) {
@@ -46,10 +48,16 @@ __device__ __forceinline__ float value_of(Key k) {
 }
 
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
-__device__ __forceinline__ Key lane_key(Key k, int lane) {
-  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(k), lane);
-  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(k >> 32), lane);
-  return (static_cast<Key>(hi) << 32) | lo;
+// A lower bound of the n-th largest of the lanes' values, 0 where there are fewer:
+// its upper 16 bits (what may reach it beside the n largest is ordered with them).
+__device__ __forceinline__ uint32_t nth_largest(uint32_t o, int n) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t u = t | (1u << bit);
+    if (__popcll(__ballot(o >= u)) >= n) t = u;
+  }
+  return t;
 }
 
 template <typename T>
@@ -98,95 +106,114 @@ __device__ __forceinline__ void load_values(const BeamArgs& a, size_t row, int t
   }
 }
 
+// EACH values of a thread.
+template <int EACH>
 __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a, Key* keys, Stat* stats) {
-  extern __shared__ Key list[];  // kGroupOf * width: no more keys reach the threshold
-  __shared__ Key tops[kWaves][64];
-  __shared__ float wave_top[kWaves];
-  __shared__ double wave_total[kWaves];
+  __shared__ float tops[kWaves][64];
+  __shared__ float sums[kThreads];
+  __shared__ Key list[kList];
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int chunk = blockIdx.x, chunks = gridDim.x;
   const size_t row = blockIdx.y;
   if (a.done != nullptr && a.done[row] != 0) return;  // its logits do not count
-  const int t0 = chunk * kChunk;
-  float v[kEach / 8][8];
+  const int t0 = chunk * (kThreads * EACH);
+  auto token = [&](int i) { return t0 + (i / 8 * kThreads + tid) * 8 + i % 8; };
+  float v[EACH / 8][8];
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i) load_values(a, row, t0 + (i * kThreads + tid) * 8, v[i]);
-  float top = -INFINITY;
-  Key best = 0;
+  for (int i = 0; i < EACH / 8; ++i) load_values(a, row, token(8 * i), v[i]);
+  float best = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = t0 + (i * kThreads + tid) * 8 + e;
-      top = fmaxf(top, v[i][e]);
-      if (t < a.vocab) best = max_key(best, key_of(v[i][e], t));
-    }
-  top = wave_max(top);
+  for (int i = 0; i < EACH; ++i) best = fmaxf(best, v[i / 8][i % 8]);
   tops[wave][lane] = best;
-  if (lane == 0) wave_top[wave] = top;
   if (tid == 0) count = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    top = fmaxf(top, wave_top[w]);
-    best = max_key(best, tops[w][lane]);
-  }
+  for (int w = 0; w < kWaves; ++w) best = fmaxf(best, tops[w][lane]);
+  const float top = wave_max(best);
+  const uint32_t least = max(nth_largest(order_of(best), a.width), order_of(-INFINITY) + 1);  // -infinity is never taken
 
   // exponentials; a NaN or an infinity leaves NaN
+  const float from = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kEach / 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += v[i][e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((v[i][e] - top) * kLog2e);
-  const double total = wave_sum(sum);
-  if (lane == 0) wave_total[wave] = total;
-
-  // The width-th largest of the 64 maxima (every wave for itself): all of the
-  // chunk's `width` best keys reach it.
-  Key least = 1;
-  int above = 0;
-  for (int l = 0; l < 64; ++l) above += lane_key(best, l) > best ? 1 : 0;
-  const uint64_t is_it = __ballot(best != 0 && above == a.width - 1);
-  if (is_it != 0) least = lane_key(best, __ffsll(static_cast<unsigned long long>(is_it)) - 1);
-#pragma unroll
-  for (int i = 0; i < kEach / 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = t0 + (i * kThreads + tid) * 8 + e;
-      const Key k = t < a.vocab ? key_of(v[i][e], t) : 0;
-      if (k >= least) list[atomicAdd(&count, 1)] = k;
+  for (int i = 0; i < EACH; ++i) {
+    const float x = v[i / 8][i % 8];
+    sum += __builtin_amdgcn_exp2f((x - from) * kLog2e);
+    const uint32_t o = order_of(x);
+    if (o >= least) {
+      const int at = atomicAdd(&count, 1);
+      if (at < kList) list[at] = (static_cast<Key>(o) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(token(i)));
     }
+  }
+  sums[tid] = sum;
   __syncthreads();
+  if (wave == kWaves - 1) {
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s += sums[w * 64 + lane];
+    s = wave_sum(s);
+    if (lane == 0) stats[row * chunks + chunk] = Stat{s, top, 0};
+  }
   const int n = count;
   Key* out = keys + (row * chunks + chunk) * a.width;
-  for (int i = tid; i < max(n, a.width); i += kThreads) {
-    if (i >= n) {
-      out[i] = 0;
-      continue;
+  if (n <= kList) {
+    for (int i = tid; i < max(n, a.width); i += kThreads) {
+      if (i >= n) {
+        out[i] = 0;
+        continue;
+      }
+      const Key k = list[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += list[j] > k ? 1 : 0;
+      if (rank < a.width) out[rank] = k;
     }
-    const Key k = list[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > k ? 1 : 0;
-    if (rank < a.width) out[rank] = k;
+    return;
   }
-  if (tid == 0) {
-    double s = wave_total[0];
-    for (int w = 1; w < kWaves; ++w) s += wave_total[w];
-    stats[row * chunks + chunk] = Stat{s, top, 0};
+  // very many equal values: the largest key below the last one, again and again
+  Key last = ~static_cast<Key>(0);
+  for (int r = 0; r < a.width; ++r) {
+    Key mine = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const Key k = token(i) < a.vocab ? key_of(v[i / 8][i % 8], token(i)) : 0;
+      if (k < last) mine = max_key(mine, k);
+    }
+    mine = wave_max(mine);
+    __syncthreads();
+    if (lane == 0) list[wave] = mine;
+    __syncthreads();
+    last = list[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) last = max_key(last, list[w]);
+    if (tid == 0) out[r] = last;
   }
 }
 
 // One workgroup per group of beams: a wave per row joins its chunks, then the
 // rows' best are ordered.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
-constexpr int kLists = chunks_of(1 << 20) / 64;  // of a lane
+constexpr int kLeastEach = 8, kMostEach = 32;
+constexpr int kJoinList = 512;                                   // keys of a wave that are ordered together
+constexpr int kLists = (1 << 20) / (kThreads * kMostEach) / 64;  // chunks of a lane, of the largest vocabulary
+
+// Values of a thread: chunks of 2048 tokens until they fill the chip (one row in
+// flight per wave hides little), of 8192 where there are many.
+int each_of(int32_t rows, int32_t vocab) {
+  const int64_t chunks = static_cast<int64_t>(rows) * ((vocab + kThreads * kLeastEach - 1) / (kThreads * kLeastEach));
+  return chunks > 8192 || vocab > (1 << 18) ? 32 : chunks > 1024 ? 16 : 8;
+}
+int chunks_of(int32_t rows, int32_t vocab) {
+  const int tokens = kThreads * each_of(rows, vocab);
+  return (vocab + tokens - 1) / tokens;
+}
 
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, const Key* keys, const Stat* stats, int chunks) {
   extern __shared__ double totals[];  // [beams][width], then their tokens
   int32_t* tokens = reinterpret_cast<int32_t*>(totals + a.beams * a.width);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int group = blockIdx.x, width = a.width;
+  __shared__ Key found[kJoinWaves][kJoinList];
   __shared__ bool ended[kMaxWidth];  // done_out may be done
   for (int b = wave; b < a.beams; b += kJoinWaves) {
     const size_t row = static_cast<size_t>(group) * a.beams + b;
@@ -210,8 +237,39 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
       if (st[c].sum != 0.0) sum += st[c].sum * exp(static_cast<double>(st[c].top) - top);
     sum = wave_sum(sum);
     const double lse = top + log(sum);
-    // the chunks' lists are in order: the largest of their heads is next
+    auto put = [&](int i, Key k) {
+      const double total = score + (static_cast<double>(value_of(k)) - lse);
+      totals[b * width + i] = k != 0 && live && total - total == 0.0 ? total : -INFINITY;
+      tokens[b * width + i] = static_cast<int32_t>(token_of(k));
+    };
     const Key* lists = keys + row * chunks * width;
+    const int all = chunks * width;
+    uint32_t best = 0;
+    for (int i = lane; i < all; i += 64) best = max(best, static_cast<uint32_t>(lists[i] >> 32));
+    const uint32_t least = max(nth_largest(best, width), 1u);
+    int n = 0;
+    for (int i0 = 0; i0 < all; i0 += 64) {
+      const Key k = i0 + lane < all ? lists[i0 + lane] : 0;
+      const bool mine = static_cast<uint32_t>(k >> 32) >= least;
+      const uint64_t which = __ballot(mine);
+      const int at = n + static_cast<int>(__popcll(which & ((1ull << lane) - 1)));
+      if (mine && at < kJoinList) found[wave][at] = k;
+      n += static_cast<int>(__popcll(which));
+    }
+    if (n <= kJoinList) {
+      for (int i = lane; i < max(n, width); i += 64) {
+        int rank = i;
+        Key k = 0;
+        if (i < n) {
+          k = found[wave][i];
+          rank = 0;
+          for (int j = 0; j < n; ++j) rank += found[wave][j] > k ? 1 : 0;
+        }
+        if (rank < width) put(rank, k);
+      }
+      continue;
+    }
+    // many equal ones: the chunks' lists are in order, the largest of their heads is next
     int at[kLists];
     Key head[kLists];
 #pragma unroll
@@ -231,21 +289,35 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
           ++at[u];
           head[u] = at[u] < width ? lists[static_cast<size_t>(lane + 64 * u) * width + at[u]] : 0;
         }
-      if (lane == 0) {
-        const double total = score + (static_cast<double>(value_of(next)) - lse);
-        totals[b * width + i] = next != 0 && live && total - total == 0.0 ? total : -INFINITY;
-        tokens[b * width + i] = static_cast<int32_t>(token_of(next));
-      }
+      if (lane == 0) put(i, next);
     }
   }
   __syncthreads();
-  // rows stand in order, and a row's tokens in the order of its totals
+  // rows stand in order, and a row's tokens in the order of its totals: how many of
+  // each row stand before a total is found by bisection
   const int n = a.beams * width;
   const size_t out = static_cast<size_t>(group) * width;
   for (int i = tid; i < n; i += kJoinThreads) {
     const double total = totals[i];
+    const int own = i / width;
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += totals[j] > total || (totals[j] == total && j < i) ? 1 : 0;
+    for (int b = 0; b < a.beams && rank < width; ++b) {
+      if (b == own) {
+        rank += i % width;
+        continue;
+      }
+      int lo = 0, hi = width;  // those below lo stand before it, those from hi on do not
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        const double t = totals[b * width + mid];
+        if (t > total || (t == total && b < own)) {
+          lo = mid + 1;
+        } else {
+          hi = mid;
+        }
+      }
+      rank += lo;
+    }
     if (rank >= width) continue;
     const bool some = total != -INFINITY;
     const size_t row = static_cast<size_t>(group) * a.beams + i / width;
@@ -259,15 +331,25 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
 
 }  // namespace
 
+// For every call with as many rows and tokens or fewer: the smallest chunks of
+// at most 8192 in all, or 4096 tokens each.
 size_t beam_ws_bytes(int32_t rows, int32_t vocab, int32_t width) {
-  return static_cast<size_t>(rows) * chunks_of(vocab) * (sizeof(Stat) + width * sizeof(Key));
+  const size_t r = rows;
+  const size_t most = std::max(r * ((vocab + 4095) / 4096), std::min<size_t>(8192 + r, r * ((vocab + 2047) / 2048)));
+  return most * (sizeof(Stat) + width * sizeof(Key));
 }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s) {
-  const int chunks = chunks_of(a.vocab);
+  const int each = each_of(a.rows, a.vocab), chunks = chunks_of(a.rows, a.vocab);
   Stat* stats = static_cast<Stat*>(a.ws);
   Key* keys = reinterpret_cast<Key*>(stats + static_cast<size_t>(a.rows) * chunks);
-  beam_chunk_kernel<<<dim3(chunks, a.rows), kThreads, sizeof(Key) * kGroupOf * a.width, s>>>(a, keys, stats);
+  const dim3 grid(chunks, a.rows);
+  if (each == 8)
+    beam_chunk_kernel<8><<<grid, kThreads, 0, s>>>(a, keys, stats);
+  else if (each == 16)
+    beam_chunk_kernel<16><<<grid, kThreads, 0, s>>>(a, keys, stats);
+  else
+    beam_chunk_kernel<32><<<grid, kThreads, 0, s>>>(a, keys, stats);
   beam_join_kernel<<<a.rows / a.beams, kJoinThreads, (sizeof(double) + sizeof(int32_t)) * a.beams * a.width, s>>>(
       a, keys, stats, chunks);
   return hipGetLastError();

@@ -549,7 +549,203 @@ PyObject* linear16(PyObject*, PyObject* const* a, Py_ssize_t n) {
       [&] { return fn(x, M, dinv, &w, y, out, s); });
 }
 
+// A matrix whose rows are contiguous, of 32 or 16 bits: pointer, row stride and type.
+bool read_matrix(PyObject* o, int64_t M, int64_t K, const void*& p, int64_t& stride, int32_t& dtype) {
+  if (o == nullptr || !THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.dim() != 2 || t.size(0) != M || t.size(1) != K || (t.stride(1) != 1 && K > 1)) return false;
+  const at::ScalarType type = t.scalar_type();
+  if (type != at::kFloat && !half(type)) return false;
+  dtype = type == at::kFloat ? SQ_OUT_F32 : half_code(type);
+  p = t.data_ptr();
+  stride = M > 1 ? t.stride(0) : (K + 7) / 8 * 8;  // one row has none
+  return true;
+}
+bool read_matrix_or_null(PyObject* o, int64_t M, int64_t K, const void*& p, int64_t& stride, int32_t& dtype) {
+  p = nullptr;
+  stride = 0;
+  dtype = 0;
+  return o == Py_None || read_matrix(o, M, K, p, stride, dtype);
+}
+bool read_size(PyObject* o, int64_t dim, int32_t d, int32_t& v) {
+  if (o == nullptr || !THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return t.dim() == dim && size32(t.size(d), v);
+}
+// The number of values of an attribute's tensor (null: no such tensor).
+bool has_values(PyObject* o, PyObject* name, int64_t n, bool optional) {
+  Attr a(o, name);
+  if (a.p == Py_None) return optional;
+  const at::Tensor* t = tensor(a.p);
+  return t != nullptr && t->dim() == 1 && t->size(0) == n;
+}
+
+// norm(address, x, residual, weight, eps, sum_out, y, out_dtype, act, qx, act_scale, stream)
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  decltype(&sq_add_rmsnorm) fn;
+  const void *x, *res, *sum;
+  int64_t xs, rs, ss;
+  int32_t M, K, xd, rd, sd, yd;
+  const float* w;
+  float eps;
+  void* y;
+  int8_t* qx;
+  float* scale;
+  sq_act_params act;
+  bool has_act;
+  hipStream_t s;
+  return guarded(
+      n, 12,
+      [&] {
+        if (!read_entry(a[0], fn) || !read_size(a[1], 2, 0, M) || !read_size(a[1], 2, 1, K) ||
+            !read_matrix(a[1], M, K, x, xs, xd) || !read_matrix_or_null(a[2], M, K, res, rs, rd) ||
+            !read_matrix_or_null(a[5], M, K, sum, ss, sd) || (sum != nullptr && (res == nullptr || sd != rd)) ||
+            !read_int(a[7], yd))
+          return false;
+        y = nullptr;
+        if (a[6] != Py_None) {
+          const at::Tensor* o = tensor(a[6]);
+          if (o == nullptr || !is_out(o->scalar_type(), yd) || !read_sized(a[6], o->scalar_type(), {M, K}, y)) return false;
+        }
+        has_act = a[8] != Py_None;
+        if (has_act && (!read(a[8], act) || !has_values(a[8], s_tok2stream, M, false) || !has_values(a[8], s_dinv, K, true)))
+          return false;
+        return read_sized_or_null(a[3], at::kFloat, {K}, w) && read_float(a[4], eps) &&
+               read_sized_or_null(a[9], at::kChar, {M, K}, qx) && read_sized_or_null(a[10], at::kFloat, {M}, scale) &&
+               read_stream(a[11], s);
+      },
+      [&] {
+        return fn(x, xs, xd, res, rs, rd, w, eps, M, K, const_cast<void*>(sum), ss, y, yd, has_act ? &act : nullptr, qx,
+                  scale, s);
+      });
+}
+
+// beams(address, logits, beams, scores, done, end_token, parent, token, score_out, done_out, workspace, stream)
+PyObject* beams(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  decltype(&sq_beam_select) fn;
+  const void* x;
+  int64_t xs;
+  int32_t R, V, xd, beams, end, width;
+  const float* scores;
+  const int32_t* done;
+  int32_t *parent, *token, *done_out;
+  float* score;
+  void* ws;
+  size_t wb;
+  hipStream_t s;
+  return guarded(
+      n, 12,
+      [&] {
+        if (!read_entry(a[0], fn) || !read_size(a[1], 2, 0, R) || !read_size(a[1], 2, 1, V) ||
+            !read_matrix(a[1], R, V, x, xs, xd) || !read_int(a[2], beams) || beams < 1 || R % beams != 0 ||
+            !read_size(a[6], 2, 1, width))
+          return false;
+        const int64_t G = R / beams;
+        return read_sized(a[3], at::kFloat, {R}, scores) && read_sized_or_null(a[4], at::kInt, {R}, done) &&
+               read_int(a[5], end) && read_sized(a[6], at::kInt, {G, width}, parent) &&
+               read_sized(a[7], at::kInt, {G, width}, token) && read_sized(a[8], at::kFloat, {G, width}, score) &&
+               read_sized_or_null(a[9], at::kInt, {G, width}, done_out) && read(a[10], ws, wb) && read_stream(a[11], s);
+      },
+      [&] {
+        return fn(x, xs, xd, R, beams, V, scores, done, end, width, parent, token, score, done_out, ws, wb, s);
+      });
+}
+
+// reorder(address, parent, kv_len, page_size, num_pages, free_pages, free_head, table, table_out, kv_len_out, copy_src,
+//         copy_dst, copy_rows, free_head_out, workspace, stream)
+PyObject* reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  decltype(&sq_kv_reorder) fn;
+  const int32_t *parent, *kv_len, *head, *table;
+  int32_t *free_pages, *table_out, *len_out, *src, *dst, *rows, *head_out;
+  int32_t R, page, num_pages, num_free, max_pages;
+  void* ws;
+  size_t wb;
+  hipStream_t s;
+  return guarded(
+      n, 16,
+      [&] {
+        return read_entry(a[0], fn) && read_size(a[7], 2, 0, R) && read_size(a[7], 2, 1, max_pages) &&
+               read_size(a[5], 1, 0, num_free) && read_sized(a[1], at::kInt, {R}, parent) &&
+               read_sized(a[2], at::kInt, {R}, kv_len) && read_int(a[3], page) && read_int(a[4], num_pages) &&
+               read_sized(a[5], at::kInt, {num_free}, free_pages) && read_sized_or_null(a[6], at::kInt, {1}, head) &&
+               read_sized(a[7], at::kInt, {R, max_pages}, table) && read_sized(a[8], at::kInt, {R, max_pages}, table_out) &&
+               read_sized(a[9], at::kInt, {R}, len_out) && read_sized(a[10], at::kInt, {R}, src) &&
+               read_sized(a[11], at::kInt, {R}, dst) && read_sized(a[12], at::kInt, {R}, rows) &&
+               read_sized(a[13], at::kInt, {1}, head_out) && read(a[14], ws, wb) && read_stream(a[15], s);
+      },
+      [&] {
+        return fn(parent, kv_len, R, page, num_pages, free_pages, num_free, head, table, max_pages, table_out, len_out, src,
+                  dst, rows, head_out, ws, wb, s);
+      });
+}
+
+// copy(address, caches, src, dst, rows, stream), caches a list or tuple of at most 64
+PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  constexpr Py_ssize_t kMost = 64;
+  decltype(&sq_kv_copy_pages) fn;
+  sq_kv_cache caches[kMost];
+  Py_ssize_t count = 0;
+  const int32_t *src, *dst, *rows;
+  int32_t entries;
+  hipStream_t s;
+  return guarded(
+      n, 6,
+      [&] {
+        if (!read_entry(a[0], fn) || (!PyList_CheckExact(a[1]) && !PyTuple_CheckExact(a[1]))) return false;
+        count = PySequence_Fast_GET_SIZE(a[1]);
+        if (count > kMost) return false;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+          at::ScalarType type;
+          if (i >= PySequence_Fast_GET_SIZE(a[1]) || !read(PySequence_Fast_GET_ITEM(a[1], i), caches[i], type)) return false;
+        }
+        return read_size(a[2], 1, 0, entries) && read_sized(a[2], at::kInt, {entries}, src) &&
+               read_sized(a[3], at::kInt, {entries}, dst) && read_sized_or_null(a[4], at::kInt, {entries}, rows) &&
+               read_stream(a[5], s);
+      },
+      [&] { return fn(caches, static_cast<int32_t>(count), src, dst, rows, entries, s); });
+}
+
+// attn_shared(address, q, kv, table, kv_len, group_start, shared_len, max_shared_len, max_own_len, scale, out, out_dtype,
+//             lse, workspace, stream)
+PyObject* attn_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  decltype(&sq_attn_shared) fn;
+  const void* q;
+  int64_t qs;
+  sq_kv_cache c;
+  const int32_t *table, *kv_len, *start, *shared;
+  int32_t R, Hq, max_pages, groups, most, mine, out_dtype;
+  float scale;
+  void *out, *ws;
+  float* lse;
+  size_t wb;
+  hipStream_t s;
+  return guarded(
+      n, 15,
+      [&] {
+        at::ScalarType type;
+        if (!read_entry(a[0], fn) || !read(a[2], c, type) || !read_size(a[3], 2, 0, R) || !read_size(a[3], 2, 1, max_pages) ||
+            !read_size(a[6], 1, 0, groups) || !read_heads(a[1], type, R, c.head_dim, q, qs, Hq) || !read_int(a[11], out_dtype))
+          return false;
+        const at::Tensor* o = tensor(a[10]);
+        if (o == nullptr || !is_out(o->scalar_type(), out_dtype)) return false;
+        return read_sized(a[10], o->scalar_type(), {R, Hq, c.head_dim}, out) &&
+               read_sized(a[3], at::kInt, {R, max_pages}, table) && read_sized(a[4], at::kInt, {R}, kv_len) &&
+               read_sized(a[5], at::kInt, {int64_t{groups} + 1}, start) && read_sized(a[6], at::kInt, {groups}, shared) &&
+               read_int(a[7], most) && read_int(a[8], mine) && read_float(a[9], scale) &&
+               read_sized_or_null(a[12], at::kFloat, {R, Hq}, lse) && read(a[13], ws, wb) && read_stream(a[14], s);
+      },
+      [&] {
+        return fn(q, qs, R, Hq, &c, table, max_pages, kv_len, start, shared, groups, most, mine, scale, out, out_dtype, lse,
+                  ws, wb, s);
+      });
+}
+
 PyMethodDef methods[] = {
+    {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm)), METH_FASTCALL, nullptr},
+    {"beams", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(beams)), METH_FASTCALL, nullptr},
+    {"reorder", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(reorder)), METH_FASTCALL, nullptr},
+    {"copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(copy)), METH_FASTCALL, nullptr},
+    {"attn_shared", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attn_shared)), METH_FASTCALL, nullptr},
     {"setup_token", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(setup_token)), METH_FASTCALL, nullptr},
     {"kv_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_plan)), METH_FASTCALL, nullptr},
     {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope)), METH_FASTCALL, nullptr},
