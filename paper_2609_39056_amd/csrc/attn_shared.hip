@@ -3,19 +3,19 @@
 // for each of its requests: the group's query rows (requests x query heads of a
 // key-value head) meet each tile of keys together.
 //
-// Three kernels: the prefix in chunks for tiles of a group's query rows, each
-// request's own tokens, and the join of both kinds of parts.  A part holds a
-// running maximum m (in units of log 2), a sum l and the weighted values.
+// Two kernels: the prefix in chunks for tiles of a group's query rows beside each
+// request's own tokens, and the join of both kinds of parts.  A part holds a running
+// maximum m (in units of log 2), a sum l and the weighted values.
 //
 // A wave takes 32 tokens at a time for Q tiles of 16 query rows, as in the paged
 // attention: scores as keys x queries, so that a lane has the probabilities that it
 // needs for the values, which it transposes in registers; nothing is passed
-// between lanes.  The waves of a workgroup take the tiles of a chunk in turn and
-// are joined through LDS.
+// between lanes.
 #include <type_traits>
 
 #include "attn_shared_split.h"
 #include "attn_tile.h"
+#include "gemm_frag.h"
 #include "token_internal.h"
 
 namespace sq {
@@ -65,103 +65,161 @@ __device__ int last_group(const SharedArgs& a, int64_t x, Place place) {
   }
 }
 
+// Four dimensions of a query head over the tokens [first, last), one after the other,
+// as the formula reads: sum of 2^(score - M) v.
+template <bool F16, int D, typename PageOf>
+__device__ float4 follow_tokens(const SharedArgs& a, int req, int head, int kvh, int first, int last, int d4, float M,
+                                PageOf page_of) {
+  const int mask = (1 << a.page_shift) - 1;
+  const float scale = a.scale * kLog2e;
+  const uint4* qr = reinterpret_cast<const uint4*>(a.q + req * a.q_stride + static_cast<size_t>(head) * D);
+  float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 1
+  for (int tok = first; tok < last; ++tok) {
+    const int page = page_of(tok);
+    if (page < 0) continue;
+    const size_t row = (((static_cast<size_t>(page) * a.Hk + kvh) << a.page_shift) + (tok & mask)) * D;
+    const uint4* kr = reinterpret_cast<const uint4*>(a.k + row);
+    float dot = 0.0f;
+#pragma unroll 1  // its registers are the kernel's
+    for (int j = 0; j < D / 8; ++j) {
+      float u[8], w8[8];
+      widen8<F16>(qr[j], u);
+      widen8<F16>(kr[j], w8);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) dot = __builtin_fmaf(u[x], w8[x], dot);
+    }
+    const uint2 raw = *reinterpret_cast<const uint2*>(a.v + row + 4 * d4);
+    add_scaled(sum, make_float4(half_lo<F16>(raw.x), half_hi<F16>(raw.x), half_lo<F16>(raw.y), half_hi<F16>(raw.y)),
+               __builtin_amdgcn_exp2f(dot * scale - M));
+  }
+  return sum;
+}
+
+// A workgroup's part of a group's prefix: query rows row0 .. row0 + rows - 1 of one
+// key-value head (row i is head kvh * each + i % each of request req0 + i / each)
+// against the tokens [begin, end), which are read through the row of request `reader`.
+struct Chunk {
+  int kvh, split, req0, row0, rows, reader, begin, end;
+};
+
+template <int ROWS>
+__device__ bool find_chunk(const SharedArgs& a, const SharedSplit& sp, uint32_t id, int each, Chunk& ch) {
+  const int lane = threadIdx.x & 63;
+  // tiles of one (key-value head, chunk) stand 8 apart: on one XCD, whose cache
+  // then has the keys and values
+  const uint32_t slots = static_cast<uint32_t>(sp.slots);
+  const uint32_t pair = id / 8 / slots * 8 + id % 8, slot = id / 8 % slots;
+  if (pair >= static_cast<uint32_t>(a.Hk * sp.count)) return false;
+  ch.kvh = static_cast<int>(pair % static_cast<uint32_t>(a.Hk));
+  ch.split = static_cast<int>(pair / static_cast<uint32_t>(a.Hk));
+  // group i has the slots from start * each / ROWS + i on, at least as many as it needs
+  auto place = [&](int i) { return static_cast<int64_t>(group_start(a, i)) * each / ROWS + i; };
+  const int group = last_group(a, slot, place);
+  const int s0 = group_start(a, group), s1 = group_start(a, group + 1);
+  ch.row0 = static_cast<int>(slot - place(group)) * ROWS;
+  if (ch.row0 < 0 || s1 <= s0 || ch.row0 >= (s1 - s0) * each) return false;
+  ch.rows = min((s1 - s0) * each - ch.row0, ROWS);
+  ch.req0 = s0;
+  const int p = shared_len(a, group);
+  const int64_t begin = static_cast<int64_t>(ch.split) * sp.chunk;
+  if (begin >= p) return false;
+  // through the first request that has the most of them
+  int stop = 0;
+  ch.reader = s0;
+  for (int m = s0; m < s1 && stop < p; m += 64) {
+    const int n = m + lane < s1 ? min(kv_len(a, m + lane), p) : 0;
+    int top = n;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
+    if (top > stop) {
+      stop = top;
+      ch.reader = m + __ffsll(static_cast<unsigned long long>(__ballot(n == top))) - 1;
+    }
+  }
+  if (begin >= stop) return false;
+  ch.begin = static_cast<int>(begin);
+  ch.end = ch.begin + min(stop - ch.begin, sp.chunk);
+  // the same in all lanes: kept in scalar registers
+  for (int* v : {&ch.kvh, &ch.split, &ch.req0, &ch.row0, &ch.rows, &ch.reader, &ch.begin, &ch.end})
+    *v = __builtin_amdgcn_readfirstlane(*v);
+  return true;
+}
+
 // Q tiles of query rows against one chunk: the prefix of a group (OWN false) or a
-// request's own tokens; probabilities as NP 16-bit parts.
+// request's own tokens; probabilities as NP 16-bit parts.  The waves take the
+// chunk's tiles of tokens in turn, keys and values straight into registers, and are
+// joined through LDS.
+template <int D, bool OWN>
+struct TokensLds {
+  float values[kWaves][kQTile][D + 4], top[kWaves][kQTile], sum[kWaves][kQTile];
+  int32_t pages[(OWN ? kAttnWhole : static_cast<int>(kSharedMost)) / kMinPage + 2];
+};
+
 template <bool F16, int D, int Q, int NP, bool OWN>
-__global__ __launch_bounds__(64 * kWaves, Q < 4 && D <= 128 ? 2 : 1) void shared_kernel(SharedArgs a, SharedSplit sp) {
+__device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSplit& sp, uint32_t id, TokensLds<D, OWN>& lds) {
   constexpr int W = kWaves;
   constexpr int KF = D / 32;  // fragments of a key row
   constexpr int E = D / 16, E0 = E < 8 ? E : 8, E1 = E - E0;  // a lane's dimensions of a value row
   constexpr int EW = E / 2;
   constexpr bool kAhead = D < 256;
-  constexpr int kPages = (OWN ? kAttnWhole : static_cast<int>(kSharedMost)) / kMinPage + 2;
   constexpr int kRows = Q * kQTile;
   constexpr float kShift = F16 ? 11.0f : 0.0f;
   constexpr float kSlack = F16 ? 4.0f : 8.0f;
-  __shared__ int32_t pages[kPages];
-  __shared__ float s_m[W][kQTile], s_l[W][kQTile], s_o[W][kQTile][D + 4];
+  int32_t* pages = lds.pages;
+  auto& s_o = lds.values;
+  auto& s_m = lds.top;
+  auto& s_l = lds.sum;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int each = a.Hq / a.Hk;
   const Parts parts = parts_of(a, sp);
 
-  // Query rows are numbered row0 ..: row i is head kvh * each + i % each of request
-  // req0 + i / each; there are `rows` of them here.
-  int kvh, split, req0, row0, rows, reader, first, stop, base, chunk;
+  Chunk ch;
+  int first = 0;
   if constexpr (OWN) {
-    const int r = blockIdx.y;
-    uint32_t wg = blockIdx.x;
     const uint32_t qtiles = static_cast<uint32_t>((each + kRows - 1) / kRows);
-    kvh = static_cast<int>(wg % static_cast<uint32_t>(a.Hk));
+    uint32_t wg = id;
+    ch.kvh = static_cast<int>(wg % static_cast<uint32_t>(a.Hk));
     wg /= static_cast<uint32_t>(a.Hk);
-    row0 = static_cast<int>(wg % qtiles) * kRows;
-    split = static_cast<int>(wg / qtiles);
+    ch.row0 = static_cast<int>(wg % qtiles) * kRows;
+    wg /= qtiles;
+    ch.split = static_cast<int>(wg % static_cast<uint32_t>(sp.mine.count));
+    const int r = static_cast<int>(wg / static_cast<uint32_t>(sp.mine.count));
     const int group = last_group(a, r, [&](int i) { return static_cast<int64_t>(group_start(a, i)); });
     const bool member = a.groups > 0 && group_start(a, group) <= r && r < group_start(a, group + 1);
     const int p = member ? shared_len(a, group) : 0;
     const int n = kv_len(a, r);
     first = min(p, n);
-    stop = static_cast<int>(min(static_cast<int64_t>(n), static_cast<int64_t>(p) + a.max_own));
-    if (blockIdx.x == 0 && threadIdx.x == 0) parts.range[r] = make_int2(first, stop);
-    reader = req0 = r;
-    rows = min(each - row0, kRows);
-    base = first & ~(kTile - 1);
-    chunk = sp.mine.chunk;
-  } else {
-    // tiles of one (key-value head, chunk) stand 8 apart: on one XCD, whose cache
-    // then has the keys and values
-    const uint32_t id = blockIdx.x, slots = static_cast<uint32_t>(sp.slots);
-    const uint32_t pair = id / 8 / slots * 8 + id % 8, slot = id / 8 % slots;
-    if (pair >= static_cast<uint32_t>(a.Hk * sp.count)) return;
-    kvh = static_cast<int>(pair % static_cast<uint32_t>(a.Hk));
-    split = static_cast<int>(pair / static_cast<uint32_t>(a.Hk));
-    // group i has the slots from start * each / rows + i on, at least as many as it needs
-    auto place = [&](int i) { return static_cast<int64_t>(group_start(a, i)) * each / kRows + i; };
-    const int group = last_group(a, slot, place);
-    const int s0 = group_start(a, group), s1 = group_start(a, group + 1);
-    row0 = static_cast<int>(slot - place(group)) * kRows;
-    if (row0 < 0 || s1 <= s0 || row0 >= (s1 - s0) * each) return;
-    rows = min((s1 - s0) * each - row0, kRows);
-    req0 = s0;
-    chunk = sp.chunk;
-    // its tokens are read through the first request that has the most of them
-    const int p = shared_len(a, group);
-    if (split * static_cast<int64_t>(chunk) >= p) return;
-    reader = s0;
-    stop = 0;
-    for (int m = s0; m < s1 && stop < p; m += 64) {
-      int n = m + lane < s1 ? min(kv_len(a, m + lane), p) : 0;
-      int top = n;
-#pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
-      if (top > stop) {
-        stop = top;
-        reader = m + __ffsll(static_cast<unsigned long long>(__ballot(n == top))) - 1;
-      }
-    }
-    first = base = 0;
+    const int stop = static_cast<int>(min(static_cast<int64_t>(n), static_cast<int64_t>(p) + a.max_own));
+    if (ch.kvh == 0 && ch.row0 == 0 && ch.split == 0 && threadIdx.x == 0) parts.range[r] = make_int2(first, stop);
+    ch.reader = ch.req0 = r;
+    ch.rows = min(each - ch.row0, kRows);
+    const int64_t begin = (first & ~(kTile - 1)) + static_cast<int64_t>(ch.split) * sp.mine.chunk;
+    if (begin >= stop) return;
+    ch.begin = static_cast<int>(begin);
+    ch.end = ch.begin + min(stop - ch.begin, sp.mine.chunk);
+  } else if (!find_chunk<kRows>(a, sp, id, each, ch)) {
+    return;
   }
-  const int64_t begin64 = base + static_cast<int64_t>(split) * chunk;
-  if (begin64 >= stop) return;
-  const int begin = static_cast<int>(begin64);
-  const int end = begin + min(stop - begin, chunk);
+  const int kvh = ch.kvh, split = ch.split, req0 = ch.req0, row0 = ch.row0, rows = ch.rows, begin = ch.begin, end = ch.end;
   const int shift = a.page_shift, mask = (1 << shift) - 1;
   const int page0 = begin >> shift, npages = ((end - 1) >> shift) - page0 + 1;
   for (int i = threadIdx.x; i < npages; i += 64 * W) {
-    const int32_t p = a.table[static_cast<size_t>(reader) * a.max_pages + page0 + i];
+    const int32_t p = a.table[static_cast<size_t>(ch.reader) * a.max_pages + page0 + i];
     pages[i] = p >= 0 && p < a.num_pages ? p : -1;
   }
 
   // queries: column c of tile y is row 16 y + c, the lane's values 32 j + 8 g ..
   uint4 q[Q][KF];
   int limit[Q];  // tokens of the rows' requests
-  int least = stop;
+  int least = end;
 #pragma unroll
   for (int y = 0; y < Q; ++y) {
     const int i = kQTile * y + c, at = row0 + min(i, rows - 1);
     const int req = req0 + at / each, head = kvh * each + at % each;
-    limit[y] = OWN ? stop : kv_len(a, req);
+    limit[y] = OWN ? end : kv_len(a, req);
     least = min(least, limit[y]);
     const uint16_t* qrow = a.q + req * a.q_stride + static_cast<size_t>(head) * D + 8 * g;
 #pragma unroll
@@ -343,32 +401,343 @@ __global__ __launch_bounds__(64 * kWaves, Q < 4 && D <= 128 ? 2 : 1) void shared
       // Parts of a probability may be 0 or negative, and 0 meets values of tokens that a
       // shorter request does not attend: where that leaves NaN the formula is followed token by token.
       if (is_nan(sum.x + sum.y + sum.z + sum.w) && !is_nan(L)) {
-        sum = make_float4(0, 0, 0, 0);
-        const uint4* qr = reinterpret_cast<const uint4*>(a.q + req * a.q_stride + static_cast<size_t>(head) * D);
-        const int last = OWN ? end : min(end, kv_len(a, req));
-        for (int tok = max(first, begin); tok < last; ++tok) {
-          const int page = page_of(tok);
-          if (page < 0) continue;
-          const size_t row = row_of(page, tok) * D;
-          const uint4* kr = reinterpret_cast<const uint4*>(a.k + row);
-          float dot = 0.0f;
-#pragma unroll 1  // its registers are the kernel's
-          for (int j = 0; j < D / 8; ++j) {
-            float u[8], w8[8];
-            widen8<F16>(qr[j], u);
-            widen8<F16>(kr[j], w8);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) dot = __builtin_fmaf(u[x], w8[x], dot);
-          }
-          const uint2 raw = *reinterpret_cast<const uint2*>(a.v + row + 4 * d4);
-          add_scaled(sum, make_float4(half_lo<F16>(raw.x), half_hi<F16>(raw.x), half_lo<F16>(raw.y), half_hi<F16>(raw.y)),
-                     __builtin_amdgcn_exp2f(dot * scale - M));
-        }
+        sum = follow_tokens<F16, D>(a, req, head, kvh, max(first, begin), OWN ? end : min(end, kv_len(a, req)), d4, M,
+                                    page_of);
       }
       const size_t part = (static_cast<size_t>(req) * a.Hq + head) * count + split;
       reinterpret_cast<float4*>(out)[part * (D / 4) + d4] = sum;
       if (d4 == 0) stat[part] = make_float2(M, L);
     }
+  }
+}
+
+// Many query rows of a group: each wave has Q tiles of 16 of them and the waves go
+// through the chunk together, so that keys and values come from memory once for 64 Q
+// rows.  They are copied 32 tokens at a time by direct global -> LDS loads into a ring
+// (SLOTS - 1 tiles ahead, one barrier per tile), in 16-byte pieces that are permuted
+// within a row so that the rows' pieces at one place fall on different banks.
+template <int D>
+struct Ring {
+  static constexpr int kPieces = D / 8;            // of a row
+  static constexpr int kTensor = kTile * 2 * D;    // bytes of a tile's keys, and of its values
+  static constexpr int kSlot = 2 * kTensor;
+  static constexpr int kSlots = D <= 128 ? 4 : D <= 192 ? 3 : 2;
+  static constexpr int kCopies = (D + 63) / 64;    // of a wave, of keys and of values, 1 KB each
+  // where piece k of row r stands in the row, and which piece stands at place k
+  static __device__ __forceinline__ int place(int r, int k) {
+    if constexpr (kPieces == 8) return k ^ ((r >> 1) & 7);
+    if constexpr (kPieces == 16 || kPieces == 32) return k ^ (r & 15);
+    const int p = k + (kPieces == 12 ? r >> 2 : r >> 1);
+    return p >= kPieces ? p - kPieces : p;
+  }
+  static __device__ __forceinline__ int piece(int r, int at) {
+    if constexpr (kPieces == 8 || kPieces == 16 || kPieces == 32) return place(r, at);
+    const int k = at - (kPieces == 12 ? r >> 2 : r >> 1);
+    return k < 0 ? k + kPieces : k;
+  }
+};
+
+// One direct global -> LDS load of 16 bytes per lane: lane i's land at `lds` + 16 i.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
+  const uint32_t m0v = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds)));
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0v), "v"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int D>
+struct RowsLds {
+  uint8_t ring[Ring<D>::kSlots][Ring<D>::kSlot];
+  int32_t pages[static_cast<int>(kSharedMost) / kMinPage + 2];
+};
+
+template <bool F16, int D, int Q, int NP>
+__device__ __forceinline__ void take_rows(const SharedArgs& a, const SharedSplit& sp, uint32_t id, RowsLds<D>& lds) {
+  using R = Ring<D>;
+  constexpr int W = kWaves;
+  constexpr int KF = D / 32;
+  constexpr int E = D / 16, E0 = E >= 8 ? 8 : 4, E1 = E - E0;  // a lane's dimensions: E0 c .., then 16 E0 + E1 c ..
+  constexpr int EW = E / 2;
+  constexpr int kRows = W * Q * kQTile;
+  constexpr float kShift = F16 ? 11.0f : 0.0f;
+  constexpr float kSlack = F16 ? 4.0f : 8.0f;
+  int32_t* pages = lds.pages;
+  auto& ring = lds.ring;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int each = a.Hq / a.Hk;
+  Chunk ch;
+  if (!find_chunk<kRows>(a, sp, id, each, ch)) return;
+  const int begin = ch.begin, end = ch.end;
+  const int shift = a.page_shift, mask = (1 << shift) - 1;
+  const int page0 = begin >> shift, npages = ((end - 1) >> shift) - page0 + 1;
+  bool pages_ok = true;
+  for (int i = threadIdx.x; i < npages; i += 64 * W) {
+    const int32_t p = a.table[static_cast<size_t>(ch.reader) * a.max_pages + page0 + i];
+    const bool ok = p >= 0 && p < a.num_pages;
+    pages[i] = ok ? p : -1;
+    pages_ok &= ok;
+  }
+  // the wave's queries (with a negative scale their negatives): column c of tile y is row 16 y + c
+  const float scale = fabsf(a.scale) * kLog2e;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  const int row0 = ch.row0 + wave * Q * kQTile, rows = min(max(ch.rows - wave * Q * kQTile, 0), Q * kQTile);
+  uint4 q[Q][KF];
+  int limit[Q];
+  int least = end;
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+    const int i = kQTile * y + c, at = i < rows ? row0 + i : ch.row0;
+    const int req = ch.req0 + at / each, head = ch.kvh * each + at % each;
+    limit[y] = kv_len(a, req);
+    if (i < rows) least = min(least, limit[y]);
+    const uint16_t* qrow = a.q + req * a.q_stride + static_cast<size_t>(head) * D + 8 * g;
+#pragma unroll
+    for (int j = 0; j < KF; ++j) {
+      q[y][j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
+      q[y][j].x ^= flip, q[y][j].y ^= flip, q[y][j].z ^= flip, q[y][j].w ^= flip;
+      if (i >= rows) q[y][j] = make_uint4(0, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
+  pages_ok = __syncthreads_and(pages_ok);
+
+  auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
+  const int tiles = (end - begin + kTile - 1) / kTile;
+  const uint32_t ring0 = lds_offset(&ring[0][0]);
+  // where a tile's pieces come from: the wave copies every fourth KB (tokens past the end repeat the last one)
+  const uint8_t *from_k[R::kCopies], *from_v[R::kCopies];
+  auto find_tile = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < R::kCopies; ++u) {
+      const int piece = min(wave + W * u, D / 16 - 1) * 64 + lane, r = piece / R::kPieces;
+      const int tok = min(begin + t * kTile + r, end - 1);
+      const size_t row = ((static_cast<size_t>(max(page_of(tok), 0)) * a.Hk + ch.kvh) << shift) + (tok & mask);
+      const size_t at = row * (2 * D) + 16 * R::piece(r, piece % R::kPieces);
+      from_k[u] = reinterpret_cast<const uint8_t*>(a.k) + at;
+      from_v[u] = reinterpret_cast<const uint8_t*>(a.v) + at;
+    }
+  };
+  auto copy_tile = [&](int slot) {
+#pragma unroll
+    for (int u = 0; u < R::kCopies; ++u) {
+      const uint32_t to = ring0 + slot * R::kSlot + min(wave + W * u, D / 16 - 1) * 1024;
+      copy16(from_k[u], to);
+      copy16(from_v[u], to + R::kTensor);
+    }
+  };
+
+  v4f o[Q][E];
+  float m[Q], l[Q];
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[y][e] = v4f{0, 0, 0, 0};
+    m[y] = kLowest;
+    l[y] = 0.0f;
+  }
+  constexpr int kAhead = R::kSlots - 1;
+  wait_vm<0>();  // (the copies are counted from here on)
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    if (u < tiles) {
+      find_tile(u);
+      copy_tile(u);
+    }
+  int slot = 0;
+  auto next_tile = [&](int t) {
+    if (t + kAhead < tiles) find_tile(t + kAhead);
+    // this tile has come (of all waves), the one before has been read (by all waves)
+    if (t + kAhead - 1 < tiles)
+      wait_vm<2 * R::kCopies * (kAhead - 1)>();
+    else
+      wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + kAhead < tiles) copy_tile(slot == 0 ? kAhead : slot - 1);
+    const uint8_t* tile = &ring[slot][0];
+    slot = slot == kAhead ? 0 : slot + 1;
+    return tile;
+  };
+  if (rows == 0) {  // a wave without rows only copies
+    for (int t = 0; t < tiles; ++t) next_tile(t);
+    return;
+  }
+  for (int t = 0; t < tiles; ++t) {
+    const uint8_t* tile = next_tile(t);
+    const int b = begin + t * kTile;
+    float f[Q][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      v4f s[Q];
+#pragma unroll
+      for (int y = 0; y < Q; ++y) s[y] = v4f{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < KF; ++j) {
+        const int r = 16 * i + c;
+        const uint4 k = *reinterpret_cast<const uint4*>(tile + r * (2 * D) + 16 * R::place(r, 4 * j + g));
+#pragma unroll
+        for (int y = 0; y < Q; ++y) s[y] = mfma<F16>(k, q[y][j], s[y]);
+      }
+#pragma unroll
+      for (int y = 0; y < Q; ++y)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[y][x];
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (the steps one after another: their operands take turns in the registers)
+    float unit = scale;  // of f, in units of log 2
+    const bool whole_tile = pages_ok && b + kTile <= least;
+    auto live = [&](int i) {
+      const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
+      return (tok < end) & (page_of(tok) >= 0);
+    };
+    if (!whole_tile) {
+      unit = 1.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
+#pragma unroll
+        for (int y = 0; y < Q; ++y) f[y][i] = (live(i) & (tok < limit[y])) ? f[y][i] * scale : -INFINITY;
+      }
+    }
+    uint32_t p[Q][NP][4];
+#pragma unroll
+    for (int y = 0; y < Q; ++y) {
+      float top = f[y][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, f[y][i]);
+      top *= unit;
+      if (__any(top > m[y] + kSlack)) {
+        const float mn = fmaxf(m[y], quad_max(top));
+        const float al = __builtin_amdgcn_exp2f(m[y] - mn);
+        m[y] = mn;
+        l[y] *= al;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[y][e] *= al;
+      }
+      const float from = kShift - m[y];
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i], unit, from));
+        float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i + 1], unit, from));
+        l[y] += x0 + x1;
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          p[y][u][i / 2] = to_half2<F16>(x0, x1);
+          if (u + 1 < NP) {
+            x0 -= half_lo<F16>(p[y][u][i / 2]);
+            x1 -= half_hi<F16>(p[y][u][i / 2]);
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t v[8][EW];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 16 * (i / 4) + 4 * g + i % 4;
+      const uint8_t* row = tile + R::kTensor + r * (2 * D);
+      auto load = [&](auto words, int first_piece, uint32_t* w) {
+        constexpr int N = decltype(words)::value;  // a lane's share of these pieces, in dwords
+        typedef unsigned int vec __attribute__((ext_vector_type(N)));
+        const vec x = *reinterpret_cast<const vec*>(row + 16 * R::place(r, first_piece + c * N / 4) + 4 * (c * N % 4));
+#pragma unroll
+        for (int z = 0; z < N; ++z) w[z] = x[z];
+      };
+      load(std::integral_constant<int, E0 / 2>{}, 0, v[i]);
+      if constexpr (E1 == 2) {
+        v[i][E0 / 2] = *reinterpret_cast<const uint32_t*>(row + 16 * R::place(r, 2 * E0 + c / 4) + 4 * (c % 4));
+      } else if constexpr (E1 > 0) {
+        load(std::integral_constant<int, E1 / 2>{}, 2 * E0, v[i] + E0 / 2);
+      }
+    }
+    if (!whole_tile) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < EW; ++w) v[i][w] = live(i) ? v[i][w] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      uint4 vt;
+      const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+      vt.x = __builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel);
+      vt.y = __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel);
+      vt.z = __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel);
+      vt.w = __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel);
+#pragma unroll
+      for (int y = 0; y < Q; ++y)
+#pragma unroll
+        for (int u = 0; u < NP; ++u)
+          o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
+    }
+  }
+
+  // The parts: column c, and the dimensions that lane 4 g + x loaded.
+  const Parts parts = parts_of(a, sp);
+  bool odd = false;
+#pragma unroll
+  for (int y = 0; y < Q; ++y) {
+    const float L = quad_sum(l[y]), M = m[y] - kShift;
+    const int i = kQTile * y + c;
+    if (i >= rows) continue;
+    const int at = row0 + i, req = ch.req0 + at / each, head = ch.kvh * each + at % each;
+    const size_t part = (static_cast<size_t>(req) * a.Hq + head) * sp.count + ch.split;
+    float* out = parts.prefix + part * D;
+    float sum = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum += o[y][e][x];
+#pragma unroll
+      for (int e = 0; e < E0; e += 4)
+        *reinterpret_cast<float4*>(out + E0 * (4 * g + x) + e) = make_float4(o[y][e][x], o[y][e + 1][x], o[y][e + 2][x], o[y][e + 3][x]);
+      if constexpr (E1 == 2) {
+        *reinterpret_cast<float2*>(out + 16 * E0 + 2 * (4 * g + x)) = make_float2(o[y][E0][x], o[y][E0 + 1][x]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E1; e += 4)
+          *reinterpret_cast<float4*>(out + 16 * E0 + E1 * (4 * g + x) + e) =
+              make_float4(o[y][E0 + e][x], o[y][E0 + e + 1][x], o[y][E0 + e + 2][x], o[y][E0 + e + 3][x]);
+      }
+    }
+    if (g == 0) parts.prefix_stat[part] = make_float2(M, L);
+    odd |= is_nan(sum) && !is_nan(L);
+  }
+  if (!__any(odd)) return;
+  // as in shared_kernel: such rows token by token, four dimensions at a time
+#pragma unroll 1
+  for (int i = 0; i < rows; ++i) {
+    const int at = row0 + i, req = ch.req0 + at / each, head = ch.kvh * each + at % each;
+    const size_t part = (static_cast<size_t>(req) * a.Hq + head) * sp.count + ch.split;
+    const float2 ml = parts.prefix_stat[part];
+    if (is_nan(ml.y)) continue;
+    if (lane < D / 4) {
+      float4* out = reinterpret_cast<float4*>(parts.prefix + part * D) + lane;
+      *out = follow_tokens<F16, D>(a, req, head, ch.kvh, begin, min(end, kv_len(a, req)), lane, ml.x,
+                                   [&](int tok) { return page_of(tok); });
+    }
+  }
+}
+
+// The prefixes' workgroups, ROWS query rows each, then those of the requests' own
+// tokens: the former compute, the latter wait for memory, and run beside them.
+template <bool F16, int D, int ROWS, int NP>
+__global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void shared_kernel(SharedArgs a, SharedSplit sp) {
+  constexpr bool kTokens = ROWS <= 2 * kQTile;
+  using Prefix = std::conditional_t<kTokens, TokensLds<D, false>, RowsLds<D>>;
+  using Own = TokensLds<D, true>;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(Prefix) > sizeof(Own) ? sizeof(Prefix) : sizeof(Own)];
+  const uint32_t id = static_cast<uint32_t>(flat_wg());
+  if (id < sp.prefix_wgs) {
+    if constexpr (kTokens)
+      take_tokens<F16, D, ROWS / kQTile, NP, false>(a, sp, id, *reinterpret_cast<Prefix*>(lds));
+    else
+      take_rows<F16, D, ROWS / kQTile / kWaves, NP>(a, sp, id, *reinterpret_cast<Prefix*>(lds));
+  } else if (id - sp.prefix_wgs < sp.own_wgs) {
+    take_tokens<F16, D, 1, 3, true>(a, sp, id - sp.prefix_wgs, *reinterpret_cast<Own*>(lds));
   }
 }
 
@@ -424,31 +793,23 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a, SharedSp
   if (d4 == 0 && a.lse != nullptr) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
-template <bool F16, int D, int Q, int NP>
-void launch_prefix(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
-  const unsigned pairs = static_cast<unsigned>((a.Hk * sp.count + 7) / 8 * 8);
-  shared_kernel<F16, D, Q, NP, false><<<pairs * static_cast<unsigned>(sp.slots), 64 * kWaves, 0, s>>>(a, sp);
+template <bool F16, int D, int NP>
+void launch_rows(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
+  const dim3 grid = wg_grid(static_cast<size_t>(sp.prefix_wgs) + sp.own_wgs);
+  switch (sp.rows) {
+    case 16: shared_kernel<F16, D, 16, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp); break;
+    case 32:
+      if constexpr (D <= 192) shared_kernel<F16, D, 32, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+      break;
+    case 64: shared_kernel<F16, D, 64, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp); break;
+    default:
+      if constexpr (D <= 128) shared_kernel<F16, D, 128, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  }
 }
 
 template <bool F16, int D>
 void launch_dim(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
-  const bool fine = a.out_dtype == SQ_OUT_F32;
-  auto prefix = [&](auto tiles) {
-    constexpr int Q = decltype(tiles)::value;
-    fine ? launch_prefix<F16, D, Q, 3>(a, sp, s) : launch_prefix<F16, D, Q, 2>(a, sp, s);
-  };
-  if (sp.count > 0 && a.groups > 0) {
-    if (sp.q == 1) {
-      prefix(std::integral_constant<int, 1>{});
-    } else if (sp.q == 2) {
-      prefix(std::integral_constant<int, 2>{});
-    } else if constexpr (D <= 128) {
-      prefix(std::integral_constant<int, kSharedTiles>{});
-    }
-  }
-  const int each = a.Hq / a.Hk;
-  const dim3 grid(a.Hk * ((each + kQTile - 1) / kQTile) * sp.mine.count, static_cast<unsigned>(a.R));
-  shared_kernel<F16, D, 1, 3, true><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  a.out_dtype == SQ_OUT_F32 ? launch_rows<F16, D, 3>(a, sp, s) : launch_rows<F16, D, 2>(a, sp, s);
 }
 
 template <bool F16>
@@ -473,9 +834,7 @@ hipError_t launch_attn_shared(const SharedArgs& a, bool f16, hipStream_t s) {
   const Parts p = parts_of(a, sp);
   const size_t used = reinterpret_cast<const char*>(p.range + a.R) - static_cast<const char*>(a.ws);
   if (used > a.ws_bytes) return hipErrorInvalidValue;
-  const int64_t wgs = static_cast<int64_t>(a.Hk * sp.count + 7) / 8 * 8 * sp.slots;
-  const int64_t mine = static_cast<int64_t>(a.Hk) * ((a.Hq / a.Hk + kQTile - 1) / kQTile) * sp.mine.count;
-  if (wgs >= (1 << 24) || mine >= (1 << 24)) return hipErrorInvalidConfiguration;  // 2^32 threads in a grid's row
+  if (shared_wgs(a.R, a.groups, a.Hq, a.Hk, sp) >= (int64_t{1} << 31)) return hipErrorInvalidConfiguration;
   f16 ? launch_type<true>(a, sp, s) : launch_type<false>(a, sp, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -1,7 +1,7 @@
 // How attention over a shared prefix is split over workgroups (host C++, no HIP).
 //
 // The prefix: query rows (requests of a group x query heads of a key-value head)
-// go in tiles of 16 to 64 per workgroup, the prefix in chunks; every part costs
+// go in tiles of 16 to 128 per workgroup, the prefix in chunks; every part costs
 // its sums in memory, so there are as few chunks as fill the CUs, of at least 128
 // tokens.  Each request's own tokens are split as in the paged attention.
 #pragma once
@@ -14,45 +14,57 @@
 
 namespace sq {
 
-constexpr int64_t kSharedWanted = 512;      // workgroups that chunks are made for
+constexpr int64_t kSharedWanted = 512;      // workgroups that fill the chip
 constexpr int64_t kSharedLeast = 128;       // tokens of a chunk, unless the prefix is shorter
 constexpr int64_t kSharedMost = 8192;
-constexpr int32_t kSharedTiles = 4;         // the most tiles of 16 query rows in a workgroup
+constexpr int32_t kSharedRows = 128;        // the most query rows of a workgroup
 
 struct SharedSplit {
-  int32_t q;                   // tiles of 16 query rows in a workgroup
+  int32_t rows;                // query rows of a workgroup: 16, 32 (waves take tokens in turn), 64 or 128 (waves share them)
   int32_t slots;               // workgroups that the query rows of a key-value head can take
   int32_t chunk, count;        // of the prefix
   AttnSplit mine;              // of a request's own tokens
+  uint32_t prefix_wgs, own_wgs;
 };
 
-// Rows of a group on one key-value head decide the tile: a tile of 64 needs that many.
-inline int32_t shared_tiles(int32_t R, int32_t groups, int32_t each, int32_t D) {
+// Workgroups of the prefixes (of whole rounds over the XCDs) and of the requests' own tokens.
+inline int64_t prefix_wgs(int32_t groups, int32_t Hk, const SharedSplit& s) {
+  return groups > 0 ? (static_cast<int64_t>(Hk) * s.count + 7) / 8 * 8 * s.slots : 0;
+}
+inline int64_t own_wgs(int32_t R, int32_t Hq, int32_t Hk, const SharedSplit& s) { return attn_heads(R, Hq, Hk) * s.mine.count; }
+inline int64_t shared_wgs(int32_t R, int32_t groups, int32_t Hq, int32_t Hk, const SharedSplit& s) {
+  return prefix_wgs(groups, Hk, s) + own_wgs(R, Hq, Hk, s);
+}
+
+// By the query rows that a group has on a key-value head.
+inline int32_t shared_rows(int32_t R, int32_t groups, int32_t each, int32_t D) {
   const int64_t rows = static_cast<int64_t>(R) * each / std::max(1, groups);
-  return rows > 32 && D <= 128 ? kSharedTiles : rows > 16 ? 2 : 1;
+  return rows > 64 && D <= 128 ? kSharedRows : rows > 32 || (rows > 16 && D > 192) ? 64 : rows > 16 ? 32 : 16;
 }
 
 inline SharedSplit shared_split(int32_t R, int32_t groups, int32_t Hq, int32_t Hk, int32_t D, int32_t max_shared,
                                 int32_t max_own) {
   SharedSplit s;
   const int32_t each = Hq / Hk;
-  s.q = shared_tiles(R, groups, each, D);
-  const int64_t rows = static_cast<int64_t>(R) * each, tile = 16 * s.q;
-  s.slots = static_cast<int32_t>(rows / tile + groups);
-  const int64_t busy = Hk * std::max<int64_t>(groups, (rows + tile - 1) / tile);
-  const int64_t want = (kSharedWanted + busy - 1) / busy;
+  s.rows = shared_rows(R, groups, each, D);
+  const int64_t rows = static_cast<int64_t>(R) * each;
+  s.slots = static_cast<int32_t>(rows / s.rows + groups);
+  const int64_t busy = Hk * std::max<int64_t>(std::max(1, groups), (rows + s.rows - 1) / s.rows);
+  const int64_t want = std::max<int64_t>(1, kSharedWanted / busy);
   const int64_t even = ((max_shared + want - 1) / want + 31) / 32 * 32;
   const int64_t chunk = std::min(kSharedMost, std::max(kSharedLeast, even));
   s.chunk = static_cast<int32_t>(chunk);
   s.count = static_cast<int32_t>((max_shared + chunk - 1) / chunk);
   s.mine = attn_split(attn_heads(R, Hq, Hk), static_cast<int64_t>(max_own) + kAttnTile - 1);
+  s.prefix_wgs = static_cast<uint32_t>(prefix_wgs(groups, Hk, s));  // (the caller refuses 2^31 or more in all)
+  s.own_wgs = static_cast<uint32_t>(own_wgs(R, Hq, Hk, s));
   return s;
 }
 
 // Parts (requests x chunks) that no batch of at most R requests with prefixes up to
-// max_shared has more of: busy is at least the requests' rows over 64.
+// max_shared has more of: busy is at least the requests' rows over 128.
 inline int64_t shared_most_parts(int64_t R, int64_t Hq, int64_t max_shared) {
-  const int64_t wanted = std::min(R * ((max_shared + kSharedLeast - 1) / kSharedLeast), kSharedWanted * 16 * kSharedTiles / Hq + 2 * R);
+  const int64_t wanted = std::min(R * ((max_shared + kSharedLeast - 1) / kSharedLeast), kSharedWanted * kSharedRows / Hq + 2 * R);
   return std::max(wanted, R * ((max_shared + kSharedMost - 1) / kSharedMost));
 }
 inline int64_t own_most_parts(int64_t R, int64_t each, int64_t max_own) {

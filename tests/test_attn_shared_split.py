@@ -17,7 +17,7 @@ int main() {
   while (scanf("%d %d %d %d %d %d %d %d %d %d", &R, &groups, &Hq, &Hk, &D, &shared, &own, &R2, &shared2, &own2) == 10) {
     const SharedSplit s = shared_split(R, groups, Hq, Hk, D, shared, own);
     const size_t used = (size_t)R * Hq * ((size_t)s.count + s.mine.count) * (D + 2) * 4 + (size_t)R * 8;
-    printf("%d %d %d %d %d %d %zu %zu %zu\\n", s.q, s.slots, s.chunk, s.count, s.mine.chunk, s.mine.count, used,
+    printf("%d %d %d %d %d %d %zu %zu %zu\\n", s.rows, s.slots, s.chunk, s.count, s.mine.chunk, s.mine.count, used,
            shared_ws_bytes(R, Hq, Hk, D, shared, own), shared_ws_bytes(R2, Hq, Hk, D, shared2, own2));
   }
 }
@@ -60,9 +60,9 @@ def cases():
 
 def test_chunks_cover_the_prefix_and_a_larger_workspace_holds_the_parts(split):
     asked = list(cases())
-    for row, (q, slots, chunk, count, mine, mines, used, need, larger) in zip(asked, split(asked)):
+    for row, (rows, slots, chunk, count, mine, mines, used, need, larger) in zip(asked, split(asked)):
         R, groups, Hq, Hk, D, shared, own = row[:7]
-        assert q in (1, 2, 4) and (D <= 128 or q <= 2), row
+        assert rows in (16, 32, 64, 128) and (D <= 128 or rows <= 64), row
         assert chunk % 32 == 0 and 128 <= chunk <= 8192 and chunk * count >= shared > chunk * (count - 1), row
         assert mine % 32 == 0 and mine <= 1280 and mine * mines >= own + 31, row  # from a multiple of 32 on
         assert used <= need <= larger, row
@@ -78,8 +78,8 @@ def test_every_group_has_the_slots_that_its_rows_need(split):
             R = sum(sizes) + before + behind
             if not 0 < R < 65536:
                 continue
-            (q, slots, *_), = split([(R, groups, Hq, Hk, D, 1000, 10, R, 1000, 10)])
-            rows, each, at = 16 * q, Hq // Hk, before
+            (rows, slots, *_), = split([(R, groups, Hq, Hk, D, 1000, 10, R, 1000, 10)])
+            each, at = Hq // Hk, before
             for g, n in enumerate(sizes):
                 first, then = at * each // rows + g, (at + n) * each // rows + g + 1
                 assert -(-n * each // rows) <= then - first
