@@ -15,7 +15,6 @@
 
 #include "attn_shared_split.h"
 #include "attn_tile.h"
-#include "gemm_frag.h"
 #include "token_internal.h"
 
 namespace sq {
@@ -150,14 +149,15 @@ __device__ bool find_chunk(const SharedArgs& a, const SharedSplit& sp, uint32_t 
 // request's own tokens; probabilities as NP 16-bit parts.  The waves take the
 // chunk's tiles of tokens in turn, keys and values straight into registers, and are
 // joined through LDS.
-template <int D, bool OWN>
-struct TokensLds {
+template <int D>
+struct Lds {
   float values[kWaves][kQTile][D + 4], top[kWaves][kQTile], sum[kWaves][kQTile];
-  int32_t pages[(OWN ? kAttnWhole : static_cast<int>(kSharedMost)) / kMinPage + 2];
+  int32_t pages[static_cast<int>(kSharedMost) / kMinPage + 2];
 };
+static_assert(kAttnWhole <= kSharedMost, "one array holds the pages of either chunk");
 
 template <bool F16, int D, int Q, int NP, bool OWN>
-__device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSplit& sp, uint32_t id, TokensLds<D, OWN>& lds) {
+__device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSplit& sp, uint32_t id, Lds<D>& lds) {
   constexpr int W = kWaves;
   constexpr int KF = D / 32;  // fragments of a key row
   constexpr int E = D / 16, E0 = E < 8 ? E : 8, E1 = E - E0;  // a lane's dimensions of a value row
@@ -206,12 +206,11 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
   const int kvh = ch.kvh, split = ch.split, req0 = ch.req0, row0 = ch.row0, rows = ch.rows, begin = ch.begin, end = ch.end;
   const int shift = a.page_shift, mask = (1 << shift) - 1;
   const int page0 = begin >> shift, npages = ((end - 1) >> shift) - page0 + 1;
-  for (int i = threadIdx.x; i < npages; i += 64 * W) {
-    const int32_t p = a.table[static_cast<size_t>(ch.reader) * a.max_pages + page0 + i];
-    pages[i] = p >= 0 && p < a.num_pages ? p : -1;
-  }
 
-  // queries: column c of tile y is row 16 y + c, the lane's values 32 j + 8 g ..
+  // queries (with a negative scale their negatives): column c of tile y is row
+  // 16 y + c, the lane's values 32 j + 8 g ..
+  const float scale = fabsf(a.scale) * kLog2e;
+  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
   uint4 q[Q][KF];
   int limit[Q];  // tokens of the rows' requests
   int least = end;
@@ -225,6 +224,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
     for (int j = 0; j < KF; ++j) {
       q[y][j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
+      q[y][j].x ^= flip, q[y][j].y ^= flip, q[y][j].z ^= flip, q[y][j].w ^= flip;
       if (i >= rows) q[y][j] = make_uint4(0, 0, 0, 0);
     }
   }
@@ -232,7 +232,14 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
   }
-  __syncthreads();
+  bool pages_ok = true;
+  for (int i = threadIdx.x; i < npages; i += 64 * W) {
+    const int32_t p = a.table[static_cast<size_t>(ch.reader) * a.max_pages + page0 + i];
+    const bool ok = p >= 0 && p < a.num_pages;
+    pages[i] = ok ? p : -1;
+    pages_ok &= ok;
+  }
+  pages_ok = __syncthreads_and(pages_ok);
 
   v4f o[Q][E];
   float m[Q], l[Q];
@@ -243,44 +250,55 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
     m[y] = kLowest;
     l[y] = 0.0f;
   }
-  const float scale = a.scale * kLog2e;
 
   auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
   auto row_of = [&](int page, int tok) {
     return ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + (tok & mask);
   };
   // a tile's keys: tokens b + 16 i + c, the lane's values 32 j + 8 g ..; its
-  // values: tokens b + 16 i + 4 g + x, the lane's dimensions.  Tokens outside
-  // [first, end) are not loaded: their lanes repeat the nearest row inside.
+  // values: tokens b + 16 i + 4 g + x, the lane's dimensions.  Where the tile lies
+  // within one page of the range its address is the same for all lanes; tokens
+  // outside [first, end) are not loaded: their lanes repeat the nearest row inside.
   const int tiles = (end - begin + kTile - 1) / kTile;
   uint4 k[2][KF];
   uint32_t v[8][EW];
-  int kp[2], vp[2];
   auto inside = [&](int b) { return b >= first && b + kTile <= end; };
+  const bool one_page = shift >= 5;
+  auto tile_row = [&](int b) {
+    const int page = __builtin_amdgcn_readfirstlane(pages[(b >> shift) - page0]);
+    return ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + (b & mask);
+  };
+  auto load_k_row = [&](int i, const uint16_t* p) {
+#pragma unroll
+    for (int j = 0; j < KF; ++j) k[i][j] = load16<OWN>(p + 32 * j);
+  };
   auto load_v_row = [&](const uint16_t* p, uint32_t* w) {
     load_words<E0 / 2, OWN>(p + E0 * c, w);
     if constexpr (E1 > 0) load_words<E1 / 2, OWN>(p + 16 * E0 + E1 * c, w + E0 / 2);
   };
   auto load_k = [&](int b) {
+    if (one_page && inside(b)) {
+      const uint16_t* p = a.k + tile_row(b) * D;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int tok = max(first, min(b + 16 * i + c, end - 1));
-      kp[i] = page_of(tok);
-      const uint16_t* p = a.k + row_of(kp[i], tok) * D + 8 * g;
+      for (int i = 0; i < 2; ++i) load_k_row(i, p + static_cast<uint32_t>((16 * i + c) * D + 8 * g));
+    } else {
 #pragma unroll
-      for (int j = 0; j < KF; ++j) k[i][j] = load16<OWN>(p + 32 * j);
+      for (int i = 0; i < 2; ++i) {
+        const int tok = max(first, min(b + 16 * i + c, end - 1));
+        load_k_row(i, a.k + row_of(page_of(tok), tok) * D + 8 * g);
+      }
     }
   };
   auto load_v = [&](int b) {
+    if (one_page && inside(b)) {
+      const uint16_t* p = a.v + tile_row(b) * D;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int tok = b + 16 * i + 4 * g, tc = max(first, min(tok, end - 1));
-      vp[i] = page_of(tc);
-      const uint16_t* p = a.v + row_of(vp[i], tc) * D;
-      if (inside(b)) {
+      for (int i = 0; i < 8; ++i) load_v_row(p + static_cast<uint32_t>((16 * (i / 4) + 4 * g + i % 4) * D), v[i]);
+    } else {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) load_v_row(p + x * D, v[4 * i + x]);
-      } else {
+      for (int i = 0; i < 2; ++i) {
+        const int tok = b + 16 * i + 4 * g, tc = max(first, min(tok, end - 1));
+        const uint16_t* p = a.v + row_of(page_of(tc), tc) * D;
 #pragma unroll
         for (int x = 0; x < 4; ++x) load_v_row(p + max(0, min(tok + x, end - 1) - tc) * D, v[4 * i + x]);
       }
@@ -305,18 +323,19 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
         for (int j = 0; j < KF; ++j) s = mfma<F16>(k[i][j], q[y][j], s);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[x] * scale;
+        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[x];
       }
     }
-    const bool whole_tile = inside(b) && b + kTile <= least && __all(kp[0] >= 0 && kp[1] >= 0);
     if (kAhead && t + W < tiles) load_k(b + W * kTile);
-    if (!whole_tile) {
+    float unit = scale;  // of f, in units of log 2
+    if (!(pages_ok && inside(b) && b + kTile <= least)) {
+      unit = 1.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
-        const bool live = (tok >= first) & (tok < end) & (vp[i / 4] >= 0);
+        const bool live = (tok >= first) & (tok < end) & (page_of(tok) >= 0);
 #pragma unroll
-        for (int y = 0; y < Q; ++y) f[y][i] = (live & (tok < limit[y])) ? f[y][i] : -INFINITY;
+        for (int y = 0; y < Q; ++y) f[y][i] = (live & (tok < limit[y])) ? f[y][i] * scale : -INFINITY;
 #pragma unroll
         for (int w = 0; w < EW; ++w) v[i][w] = live ? v[i][w] : 0;
       }
@@ -327,6 +346,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
       float top = f[y][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, f[y][i]);
+      top *= unit;
       if (__any(top > m[y] + kSlack)) {
         const float mn = fmaxf(m[y], quad_max(top));
         const float al = __builtin_amdgcn_exp2f(m[y] - mn);
@@ -335,16 +355,19 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
         for (int e = 0; e < E; ++e) o[y][e] *= al;
       }
-      const float from = m[y] - kShift;
+      const float from = kShift - m[y];
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        float x0 = __builtin_amdgcn_exp2f(f[y][i] - from), x1 = __builtin_amdgcn_exp2f(f[y][i + 1] - from);
+        float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i], unit, from));
+        float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i + 1], unit, from));
         l[y] += x0 + x1;
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
           p[y][u][i / 2] = to_half2<F16>(x0, x1);
-          x0 -= half_lo<F16>(p[y][u][i / 2]);
-          x1 -= half_hi<F16>(p[y][u][i / 2]);
+          if (u + 1 < NP) {
+            x0 -= half_lo<F16>(p[y][u][i / 2]);
+            x1 -= half_hi<F16>(p[y][u][i / 2]);
+          }
         }
       }
     }
@@ -411,334 +434,16 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
   }
 }
 
-// Many query rows of a group: each wave has Q tiles of 16 of them and the waves go
-// through the chunk together, so that keys and values come from memory once for 64 Q
-// rows.  They are copied 32 tokens at a time by direct global -> LDS loads into a ring
-// (SLOTS - 1 tiles ahead, one barrier per tile), in 16-byte pieces that are permuted
-// within a row so that the rows' pieces at one place fall on different banks.
-template <int D>
-struct Ring {
-  static constexpr int kPieces = D / 8;            // of a row
-  static constexpr int kTensor = kTile * 2 * D;    // bytes of a tile's keys, and of its values
-  static constexpr int kSlot = 2 * kTensor;
-  static constexpr int kSlots = D <= 128 ? 4 : D <= 192 ? 3 : 2;
-  static constexpr int kCopies = (D + 63) / 64;    // of a wave, of keys and of values, 1 KB each
-  // where piece k of row r stands in the row, and which piece stands at place k
-  static __device__ __forceinline__ int place(int r, int k) {
-    if constexpr (kPieces == 8) return k ^ ((r >> 1) & 7);
-    if constexpr (kPieces == 16 || kPieces == 32) return k ^ (r & 15);
-    const int p = k + (kPieces == 12 ? r >> 2 : r >> 1);
-    return p >= kPieces ? p - kPieces : p;
-  }
-  static __device__ __forceinline__ int piece(int r, int at) {
-    if constexpr (kPieces == 8 || kPieces == 16 || kPieces == 32) return place(r, at);
-    const int k = at - (kPieces == 12 ? r >> 2 : r >> 1);
-    return k < 0 ? k + kPieces : k;
-  }
-};
-
-// One direct global -> LDS load of 16 bytes per lane: lane i's land at `lds` + 16 i.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
-  const uint32_t m0v = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds)));
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0v), "v"(from) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-template <int D>
-struct RowsLds {
-  uint8_t ring[Ring<D>::kSlots][Ring<D>::kSlot];
-  int32_t pages[static_cast<int>(kSharedMost) / kMinPage + 2];
-};
-
-template <bool F16, int D, int Q, int NP>
-__device__ __forceinline__ void take_rows(const SharedArgs& a, const SharedSplit& sp, uint32_t id, RowsLds<D>& lds) {
-  using R = Ring<D>;
-  constexpr int W = kWaves;
-  constexpr int KF = D / 32;
-  constexpr int E = D / 16, E0 = E >= 8 ? 8 : 4, E1 = E - E0;  // a lane's dimensions: E0 c .., then 16 E0 + E1 c ..
-  constexpr int EW = E / 2;
-  constexpr int kRows = W * Q * kQTile;
-  constexpr float kShift = F16 ? 11.0f : 0.0f;
-  constexpr float kSlack = F16 ? 4.0f : 8.0f;
-  int32_t* pages = lds.pages;
-  auto& ring = lds.ring;
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4;
-  const int each = a.Hq / a.Hk;
-  Chunk ch;
-  if (!find_chunk<kRows>(a, sp, id, each, ch)) return;
-  const int begin = ch.begin, end = ch.end;
-  const int shift = a.page_shift, mask = (1 << shift) - 1;
-  const int page0 = begin >> shift, npages = ((end - 1) >> shift) - page0 + 1;
-  bool pages_ok = true;
-  for (int i = threadIdx.x; i < npages; i += 64 * W) {
-    const int32_t p = a.table[static_cast<size_t>(ch.reader) * a.max_pages + page0 + i];
-    const bool ok = p >= 0 && p < a.num_pages;
-    pages[i] = ok ? p : -1;
-    pages_ok &= ok;
-  }
-  // the wave's queries (with a negative scale their negatives): column c of tile y is row 16 y + c
-  const float scale = fabsf(a.scale) * kLog2e;
-  const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
-  const int row0 = ch.row0 + wave * Q * kQTile, rows = min(max(ch.rows - wave * Q * kQTile, 0), Q * kQTile);
-  uint4 q[Q][KF];
-  int limit[Q];
-  int least = end;
-#pragma unroll
-  for (int y = 0; y < Q; ++y) {
-    const int i = kQTile * y + c, at = i < rows ? row0 + i : ch.row0;
-    const int req = ch.req0 + at / each, head = ch.kvh * each + at % each;
-    limit[y] = kv_len(a, req);
-    if (i < rows) least = min(least, limit[y]);
-    const uint16_t* qrow = a.q + req * a.q_stride + static_cast<size_t>(head) * D + 8 * g;
-#pragma unroll
-    for (int j = 0; j < KF; ++j) {
-      q[y][j] = *reinterpret_cast<const uint4*>(qrow + 32 * j);
-      q[y][j].x ^= flip, q[y][j].y ^= flip, q[y][j].z ^= flip, q[y][j].w ^= flip;
-      if (i >= rows) q[y][j] = make_uint4(0, 0, 0, 0);
-    }
-  }
-#pragma unroll
-  for (int o = 8; o >= 1; o >>= 1) least = min(least, __shfl_xor(least, o, 64));
-  pages_ok = __syncthreads_and(pages_ok);
-
-  auto page_of = [&](int tok) { return pages[max(0, min((tok >> shift) - page0, npages - 1))]; };
-  const int tiles = (end - begin + kTile - 1) / kTile;
-  const uint32_t ring0 = lds_offset(&ring[0][0]);
-  // where a tile's pieces come from: the wave copies every fourth KB (tokens past the end repeat the last one)
-  const uint8_t *from_k[R::kCopies], *from_v[R::kCopies];
-  auto find_tile = [&](int t) {
-#pragma unroll
-    for (int u = 0; u < R::kCopies; ++u) {
-      const int piece = min(wave + W * u, D / 16 - 1) * 64 + lane, r = piece / R::kPieces;
-      const int tok = min(begin + t * kTile + r, end - 1);
-      const size_t row = ((static_cast<size_t>(max(page_of(tok), 0)) * a.Hk + ch.kvh) << shift) + (tok & mask);
-      const size_t at = row * (2 * D) + 16 * R::piece(r, piece % R::kPieces);
-      from_k[u] = reinterpret_cast<const uint8_t*>(a.k) + at;
-      from_v[u] = reinterpret_cast<const uint8_t*>(a.v) + at;
-    }
-  };
-  auto copy_tile = [&](int slot) {
-#pragma unroll
-    for (int u = 0; u < R::kCopies; ++u) {
-      const uint32_t to = ring0 + slot * R::kSlot + min(wave + W * u, D / 16 - 1) * 1024;
-      copy16(from_k[u], to);
-      copy16(from_v[u], to + R::kTensor);
-    }
-  };
-
-  v4f o[Q][E];
-  float m[Q], l[Q];
-#pragma unroll
-  for (int y = 0; y < Q; ++y) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[y][e] = v4f{0, 0, 0, 0};
-    m[y] = kLowest;
-    l[y] = 0.0f;
-  }
-  constexpr int kAhead = R::kSlots - 1;
-  wait_vm<0>();  // (the copies are counted from here on)
-#pragma unroll
-  for (int u = 0; u < kAhead; ++u)
-    if (u < tiles) {
-      find_tile(u);
-      copy_tile(u);
-    }
-  int slot = 0;
-  auto next_tile = [&](int t) {
-    if (t + kAhead < tiles) find_tile(t + kAhead);
-    // this tile has come (of all waves), the one before has been read (by all waves)
-    if (t + kAhead - 1 < tiles)
-      wait_vm<2 * R::kCopies * (kAhead - 1)>();
-    else
-      wait_vm<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + kAhead < tiles) copy_tile(slot == 0 ? kAhead : slot - 1);
-    const uint8_t* tile = &ring[slot][0];
-    slot = slot == kAhead ? 0 : slot + 1;
-    return tile;
-  };
-  if (rows == 0) {  // a wave without rows only copies
-    for (int t = 0; t < tiles; ++t) next_tile(t);
-    return;
-  }
-  for (int t = 0; t < tiles; ++t) {
-    const uint8_t* tile = next_tile(t);
-    const int b = begin + t * kTile;
-    float f[Q][8];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      v4f s[Q];
-#pragma unroll
-      for (int y = 0; y < Q; ++y) s[y] = v4f{0, 0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < KF; ++j) {
-        const int r = 16 * i + c;
-        const uint4 k = *reinterpret_cast<const uint4*>(tile + r * (2 * D) + 16 * R::place(r, 4 * j + g));
-#pragma unroll
-        for (int y = 0; y < Q; ++y) s[y] = mfma<F16>(k, q[y][j], s[y]);
-      }
-#pragma unroll
-      for (int y = 0; y < Q; ++y)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[y][x];
-    }
-    __builtin_amdgcn_sched_barrier(0);  // (the steps one after another: their operands take turns in the registers)
-    float unit = scale;  // of f, in units of log 2
-    const bool whole_tile = pages_ok && b + kTile <= least;
-    auto live = [&](int i) {
-      const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
-      return (tok < end) & (page_of(tok) >= 0);
-    };
-    if (!whole_tile) {
-      unit = 1.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int tok = b + 16 * (i / 4) + 4 * g + i % 4;
-#pragma unroll
-        for (int y = 0; y < Q; ++y) f[y][i] = (live(i) & (tok < limit[y])) ? f[y][i] * scale : -INFINITY;
-      }
-    }
-    uint32_t p[Q][NP][4];
-#pragma unroll
-    for (int y = 0; y < Q; ++y) {
-      float top = f[y][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) top = fmaxf(top, f[y][i]);
-      top *= unit;
-      if (__any(top > m[y] + kSlack)) {
-        const float mn = fmaxf(m[y], quad_max(top));
-        const float al = __builtin_amdgcn_exp2f(m[y] - mn);
-        m[y] = mn;
-        l[y] *= al;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[y][e] *= al;
-      }
-      const float from = kShift - m[y];
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i], unit, from));
-        float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i + 1], unit, from));
-        l[y] += x0 + x1;
-#pragma unroll
-        for (int u = 0; u < NP; ++u) {
-          p[y][u][i / 2] = to_half2<F16>(x0, x1);
-          if (u + 1 < NP) {
-            x0 -= half_lo<F16>(p[y][u][i / 2]);
-            x1 -= half_hi<F16>(p[y][u][i / 2]);
-          }
-        }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    uint32_t v[8][EW];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 16 * (i / 4) + 4 * g + i % 4;
-      const uint8_t* row = tile + R::kTensor + r * (2 * D);
-      auto load = [&](auto words, int first_piece, uint32_t* w) {
-        constexpr int N = decltype(words)::value;  // a lane's share of these pieces, in dwords
-        typedef unsigned int vec __attribute__((ext_vector_type(N)));
-        const vec x = *reinterpret_cast<const vec*>(row + 16 * R::place(r, first_piece + c * N / 4) + 4 * (c * N % 4));
-#pragma unroll
-        for (int z = 0; z < N; ++z) w[z] = x[z];
-      };
-      load(std::integral_constant<int, E0 / 2>{}, 0, v[i]);
-      if constexpr (E1 == 2) {
-        v[i][E0 / 2] = *reinterpret_cast<const uint32_t*>(row + 16 * R::place(r, 2 * E0 + c / 4) + 4 * (c % 4));
-      } else if constexpr (E1 > 0) {
-        load(std::integral_constant<int, E1 / 2>{}, 2 * E0, v[i] + E0 / 2);
-      }
-    }
-    if (!whole_tile) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int w = 0; w < EW; ++w) v[i][w] = live(i) ? v[i][w] : 0;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      uint4 vt;
-      const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-      vt.x = __builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], sel);
-      vt.y = __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], sel);
-      vt.z = __builtin_amdgcn_perm(v[5][e / 2], v[4][e / 2], sel);
-      vt.w = __builtin_amdgcn_perm(v[7][e / 2], v[6][e / 2], sel);
-#pragma unroll
-      for (int y = 0; y < Q; ++y)
-#pragma unroll
-        for (int u = 0; u < NP; ++u)
-          o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
-    }
-  }
-
-  // The parts: column c, and the dimensions that lane 4 g + x loaded.
-  const Parts parts = parts_of(a, sp);
-  bool odd = false;
-#pragma unroll
-  for (int y = 0; y < Q; ++y) {
-    const float L = quad_sum(l[y]), M = m[y] - kShift;
-    const int i = kQTile * y + c;
-    if (i >= rows) continue;
-    const int at = row0 + i, req = ch.req0 + at / each, head = ch.kvh * each + at % each;
-    const size_t part = (static_cast<size_t>(req) * a.Hq + head) * sp.count + ch.split;
-    float* out = parts.prefix + part * D;
-    float sum = 0.0f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum += o[y][e][x];
-#pragma unroll
-      for (int e = 0; e < E0; e += 4)
-        *reinterpret_cast<float4*>(out + E0 * (4 * g + x) + e) = make_float4(o[y][e][x], o[y][e + 1][x], o[y][e + 2][x], o[y][e + 3][x]);
-      if constexpr (E1 == 2) {
-        *reinterpret_cast<float2*>(out + 16 * E0 + 2 * (4 * g + x)) = make_float2(o[y][E0][x], o[y][E0 + 1][x]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E1; e += 4)
-          *reinterpret_cast<float4*>(out + 16 * E0 + E1 * (4 * g + x) + e) =
-              make_float4(o[y][E0 + e][x], o[y][E0 + e + 1][x], o[y][E0 + e + 2][x], o[y][E0 + e + 3][x]);
-      }
-    }
-    if (g == 0) parts.prefix_stat[part] = make_float2(M, L);
-    odd |= is_nan(sum) && !is_nan(L);
-  }
-  if (!__any(odd)) return;
-  // as in shared_kernel: such rows token by token, four dimensions at a time
-#pragma unroll 1
-  for (int i = 0; i < rows; ++i) {
-    const int at = row0 + i, req = ch.req0 + at / each, head = ch.kvh * each + at % each;
-    const size_t part = (static_cast<size_t>(req) * a.Hq + head) * sp.count + ch.split;
-    const float2 ml = parts.prefix_stat[part];
-    if (is_nan(ml.y)) continue;
-    if (lane < D / 4) {
-      float4* out = reinterpret_cast<float4*>(parts.prefix + part * D) + lane;
-      *out = follow_tokens<F16, D>(a, req, head, ch.kvh, begin, min(end, kv_len(a, req)), lane, ml.x,
-                                   [&](int tok) { return page_of(tok); });
-    }
-  }
-}
-
 // The prefixes' workgroups, ROWS query rows each, then those of the requests' own
 // tokens: the former compute, the latter wait for memory, and run beside them.
 template <bool F16, int D, int ROWS, int NP>
 __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void shared_kernel(SharedArgs a, SharedSplit sp) {
-  constexpr bool kTokens = ROWS <= 2 * kQTile;
-  using Prefix = std::conditional_t<kTokens, TokensLds<D, false>, RowsLds<D>>;
-  using Own = TokensLds<D, true>;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[sizeof(Prefix) > sizeof(Own) ? sizeof(Prefix) : sizeof(Own)];
+  __shared__ Lds<D> lds;
   const uint32_t id = static_cast<uint32_t>(flat_wg());
-  if (id < sp.prefix_wgs) {
-    if constexpr (kTokens)
-      take_tokens<F16, D, ROWS / kQTile, NP, false>(a, sp, id, *reinterpret_cast<Prefix*>(lds));
-    else
-      take_rows<F16, D, ROWS / kQTile / kWaves, NP>(a, sp, id, *reinterpret_cast<Prefix*>(lds));
-  } else if (id - sp.prefix_wgs < sp.own_wgs) {
-    take_tokens<F16, D, 1, 3, true>(a, sp, id - sp.prefix_wgs, *reinterpret_cast<Own*>(lds));
-  }
+  if (id < sp.prefix_wgs)
+    take_tokens<F16, D, ROWS / kQTile, NP, false>(a, sp, id, lds);
+  else if (id - sp.prefix_wgs < sp.own_wgs)
+    take_tokens<F16, D, 1, 3, true>(a, sp, id - sp.prefix_wgs, lds);
 }
 
 // Joins the parts of a query head: a thread takes four dimensions.
@@ -796,14 +501,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a, SharedSp
 template <bool F16, int D, int NP>
 void launch_rows(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
   const dim3 grid = wg_grid(static_cast<size_t>(sp.prefix_wgs) + sp.own_wgs);
-  switch (sp.rows) {
-    case 16: shared_kernel<F16, D, 16, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp); break;
-    case 32:
-      if constexpr (D <= 192) shared_kernel<F16, D, 32, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
-      break;
-    case 64: shared_kernel<F16, D, 64, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp); break;
-    default:
-      if constexpr (D <= 128) shared_kernel<F16, D, 128, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  if (sp.rows == 16) {
+    shared_kernel<F16, D, 16, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  } else if constexpr (D <= 192) {
+    shared_kernel<F16, D, 32, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
   }
 }
 

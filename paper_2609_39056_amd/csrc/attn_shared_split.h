@@ -1,9 +1,18 @@
 // How attention over a shared prefix is split over workgroups (host C++, no HIP).
 //
 // The prefix: query rows (requests of a group x query heads of a key-value head)
-// go in tiles of 16 to 128 per workgroup, the prefix in chunks; every part costs
-// its sums in memory, so there are as few chunks as fill the CUs, of at least 128
-// tokens.  Each request's own tokens are split as in the paged attention.
+// go in tiles of 16 or 32 per workgroup, the prefix in chunks; every part costs
+// its sums in memory, so there are as few chunks as fill the CUs beside the
+// workgroups of the requests' own tokens, of at least 128 tokens.  Those are split as
+// in the paged attention.
+//
+// 384 workgroups (64 rows of 5 heads on 8 by 8192 tokens 50.6 us, 24 groups of 56 rows
+// by up to 4001 26.5, 64 rows on 8 by 32768 48.6, 16 groups of 20 rows on 8 by up to
+// 2048 25.4) are near the best everywhere: 256 take 49.0, 30.5, 54.2 and 27.1, 512 58.9,
+// 25.7, 56.0 and 27.4.  Past head dimension 128 registers leave one workgroup per CU:
+// 256 (32 rows of 8 heads of 256 by 4096 28.1 us, with 384 32.6).  Tiles of 64 rows were
+// slower in every form tried: sums in accumulation registers (the first of these 70 us),
+// keys and values through LDS for four waves of 16 or 32 rows (56 and 53).
 #pragma once
 
 #include <stdint.h>
@@ -14,13 +23,13 @@
 
 namespace sq {
 
-constexpr int64_t kSharedWanted = 512;      // workgroups that fill the chip
+constexpr int64_t kSharedWanted = 384;      // workgroups that chunks are made for
 constexpr int64_t kSharedLeast = 128;       // tokens of a chunk, unless the prefix is shorter
 constexpr int64_t kSharedMost = 8192;
-constexpr int32_t kSharedRows = 128;        // the most query rows of a workgroup
+constexpr int32_t kSharedRows = 32;         // the most query rows of a workgroup
 
 struct SharedSplit {
-  int32_t rows;                // query rows of a workgroup: 16, 32 (waves take tokens in turn), 64 or 128 (waves share them)
+  int32_t rows;                // query rows of a workgroup: 16 or 32
   int32_t slots;               // workgroups that the query rows of a key-value head can take
   int32_t chunk, count;        // of the prefix
   AttnSplit mine;              // of a request's own tokens
@@ -39,7 +48,7 @@ inline int64_t shared_wgs(int32_t R, int32_t groups, int32_t Hq, int32_t Hk, con
 // By the query rows that a group has on a key-value head.
 inline int32_t shared_rows(int32_t R, int32_t groups, int32_t each, int32_t D) {
   const int64_t rows = static_cast<int64_t>(R) * each / std::max(1, groups);
-  return rows > 64 && D <= 128 ? kSharedRows : rows > 32 || (rows > 16 && D > 192) ? 64 : rows > 16 ? 32 : 16;
+  return rows > 16 && D <= 192 ? kSharedRows : 16;
 }
 
 inline SharedSplit shared_split(int32_t R, int32_t groups, int32_t Hq, int32_t Hk, int32_t D, int32_t max_shared,
@@ -50,7 +59,7 @@ inline SharedSplit shared_split(int32_t R, int32_t groups, int32_t Hq, int32_t H
   const int64_t rows = static_cast<int64_t>(R) * each;
   s.slots = static_cast<int32_t>(rows / s.rows + groups);
   const int64_t busy = Hk * std::max<int64_t>(std::max(1, groups), (rows + s.rows - 1) / s.rows);
-  const int64_t want = std::max<int64_t>(1, kSharedWanted / busy);
+  const int64_t want = std::max<int64_t>(1, (D <= 128 ? kSharedWanted : 256) / busy);
   const int64_t even = ((max_shared + want - 1) / want + 31) / 32 * 32;
   const int64_t chunk = std::min(kSharedMost, std::max(kSharedLeast, even));
   s.chunk = static_cast<int32_t>(chunk);
@@ -62,7 +71,7 @@ inline SharedSplit shared_split(int32_t R, int32_t groups, int32_t Hq, int32_t H
 }
 
 // Parts (requests x chunks) that no batch of at most R requests with prefixes up to
-// max_shared has more of: busy is at least the requests' rows over 128.
+// max_shared has more of: busy is at least the requests' rows over 32.
 inline int64_t shared_most_parts(int64_t R, int64_t Hq, int64_t max_shared) {
   const int64_t wanted = std::min(R * ((max_shared + kSharedLeast - 1) / kSharedLeast), kSharedWanted * kSharedRows / Hq + 2 * R);
   return std::max(wanted, R * ((max_shared + kSharedMost - 1) / kSharedMost));

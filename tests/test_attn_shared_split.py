@@ -62,7 +62,7 @@ def test_chunks_cover_the_prefix_and_a_larger_workspace_holds_the_parts(split):
     asked = list(cases())
     for row, (rows, slots, chunk, count, mine, mines, used, need, larger) in zip(asked, split(asked)):
         R, groups, Hq, Hk, D, shared, own = row[:7]
-        assert rows in (16, 32, 64, 128) and (D <= 128 or rows <= 64), row
+        assert rows in (16, 32) and (D <= 192 or rows == 16), row
         assert chunk % 32 == 0 and 128 <= chunk <= 8192 and chunk * count >= shared > chunk * (count - 1), row
         assert mine % 32 == 0 and mine <= 1280 and mine * mines >= own + 31, row  # from a multiple of 32 on
         assert used <= need <= larger, row
