@@ -42,10 +42,10 @@ __device__ __forceinline__ Key key_of(float v, uint32_t token) {
   return (static_cast<Key>(order_of(v)) << 32) | (0xFFFFFFFFu - token);
 }
 __device__ __forceinline__ uint32_t token_of(Key k) { return 0xFFFFFFFFu - static_cast<uint32_t>(k); }
-__device__ __forceinline__ float value_of(Key k) {
-  const uint32_t o = static_cast<uint32_t>(k >> 32);
+__device__ __forceinline__ float value_of_order(uint32_t o) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
+__device__ __forceinline__ float value_of(Key k) { return value_of_order(static_cast<uint32_t>(k >> 32)); }
 
 __device__ __forceinline__ Key max_key(Key a, Key b) { return a > b ? a : b; }
 // A lower bound of the n-th largest of the lanes' values, 0 where there are fewer:
@@ -131,7 +131,8 @@ __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a, Key* k
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) best = fmaxf(best, tops[w][lane]);
   const float top = wave_max(best);
-  const uint32_t least = max(nth_largest(order_of(best), a.width), order_of(-INFINITY) + 1);  // -infinity is never taken
+  // (-infinity is never taken)
+  const float least = value_of_order(max(nth_largest(order_of(best), a.width), order_of(-INFINITY) + 1));
 
   // exponentials; a NaN or an infinity leaves NaN
   const float from = top == -INFINITY ? 0.0f : top;
@@ -140,10 +141,9 @@ __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a, Key* k
   for (int i = 0; i < EACH; ++i) {
     const float x = v[i / 8][i % 8];
     sum += __builtin_amdgcn_exp2f((x - from) * kLog2e);
-    const uint32_t o = order_of(x);
-    if (o >= least) {
+    if (x >= least) {
       const int at = atomicAdd(&count, 1);
-      if (at < kList) list[at] = (static_cast<Key>(o) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(token(i)));
+      if (at < kList) list[at] = key_of(x, token(i));
     }
   }
   sums[tid] = sum;
@@ -165,6 +165,7 @@ __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a, Key* k
       }
       const Key k = list[i];
       int rank = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) rank += list[j] > k ? 1 : 0;
       if (rank < a.width) out[rank] = k;
     }
@@ -197,14 +198,20 @@ constexpr int kLeastEach = 8, kMostEach = 32;
 constexpr int kJoinList = 512;                                   // keys of a wave that are ordered together
 constexpr int kLists = (1 << 20) / (kThreads * kMostEach) / 64;  // chunks of a lane, of the largest vocabulary
 
-// Values of a thread: chunks of 2048 tokens until they fill the chip (one row in
-// flight per wave hides little), of 8192 where there are many.
-int each_of(int32_t rows, int32_t vocab) {
-  const int64_t chunks = static_cast<int64_t>(rows) * ((vocab + kThreads * kLeastEach - 1) / (kThreads * kLeastEach));
-  return chunks > 8192 || vocab > (1 << 18) ? 32 : chunks > 1024 ? 16 : 8;
+// Values of a thread.  Short chunks fill the chip where there is little to read, but
+// leave more keys to join: 2048 tokens up to 1024 chunks, 4096 up to 8192, and longer
+// ones where a row would leave more than 256 keys (128 rows of 131071, 8 each: 24.1,
+// 20.9 and 20.0 us with 2048, 4096 and 8192 tokens; 8 rows, 16 each: 24.6, 19.3, 15.9;
+// 64 rows of 32000, 4 each: 10.1, 10.1, 10.9).
+int each_of(int32_t rows, int32_t vocab, int32_t width) {
+  auto chunks = [&](int each) { return static_cast<int64_t>((vocab + kThreads * each - 1) / (kThreads * each)); };
+  int each = vocab > (1 << 18) ? 32 : kLeastEach;
+  if (each == 8 && (rows * chunks(8) > 1024 || chunks(8) * width > 256)) each = 16;
+  if (each == 16 && (rows * chunks(8) > 8192 || chunks(16) * width > 256)) each = 32;
+  return each;
 }
-int chunks_of(int32_t rows, int32_t vocab) {
-  const int tokens = kThreads * each_of(rows, vocab);
+int chunks_of(int32_t rows, int32_t vocab, int32_t width) {
+  const int tokens = kThreads * each_of(rows, vocab, width);
   return (vocab + tokens - 1) / tokens;
 }
 
@@ -229,12 +236,19 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
       continue;
     }
     const Stat* st = stats + row * chunks;
+    Stat part[kLists];
     float top = -INFINITY;
-    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, st[c].top);
+#pragma unroll
+    for (int u = 0; u < kLists; ++u) {
+      const int c = lane + 64 * u;
+      part[u] = c < chunks ? st[c] : Stat{0.0, -INFINITY, 0};
+      top = fmaxf(top, part[u].top);
+    }
     top = wave_max(top);
     double sum = 0.0;
-    for (int c = lane; c < chunks; c += 64)
-      if (st[c].sum != 0.0) sum += st[c].sum * exp(static_cast<double>(st[c].top) - top);
+#pragma unroll
+    for (int u = 0; u < kLists; ++u)
+      if (part[u].sum != 0.0) sum += part[u].sum * exp(static_cast<double>(part[u].top) - top);
     sum = wave_sum(sum);
     const double lse = top + log(sum);
     auto put = [&](int i, Key k) {
@@ -244,18 +258,27 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
     };
     const Key* lists = keys + row * chunks * width;
     const int all = chunks * width;
+    // up to 512 keys stay in registers between the threshold and the list
+    constexpr int kHold = 8;
+    Key held[kHold];
     uint32_t best = 0;
-    for (int i = lane; i < all; i += 64) best = max(best, static_cast<uint32_t>(lists[i] >> 32));
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) held[u] = lane + 64 * u < all ? lists[lane + 64 * u] : 0;
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) best = max(best, static_cast<uint32_t>(held[u] >> 32));
+    for (int i = lane + 64 * kHold; i < all; i += 64) best = max(best, static_cast<uint32_t>(lists[i] >> 32));
     const uint32_t least = max(nth_largest(best, width), 1u);
     int n = 0;
-    for (int i0 = 0; i0 < all; i0 += 64) {
-      const Key k = i0 + lane < all ? lists[i0 + lane] : 0;
+    auto keep = [&](Key k) {
       const bool mine = static_cast<uint32_t>(k >> 32) >= least;
       const uint64_t which = __ballot(mine);
       const int at = n + static_cast<int>(__popcll(which & ((1ull << lane) - 1)));
       if (mine && at < kJoinList) found[wave][at] = k;
       n += static_cast<int>(__popcll(which));
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < kHold; ++u) keep(held[u]);
+    for (int i0 = 64 * kHold; i0 < all; i0 += 64) keep(i0 + lane < all ? lists[i0 + lane] : 0);
     if (n <= kJoinList) {
       for (int i = lane; i < max(n, width); i += 64) {
         int rank = i;
@@ -263,6 +286,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
         if (i < n) {
           k = found[wave][i];
           rank = 0;
+#pragma unroll 8
           for (int j = 0; j < n; ++j) rank += found[wave][j] > k ? 1 : 0;
         }
         if (rank < width) put(rank, k);
@@ -293,15 +317,19 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
     }
   }
   __syncthreads();
-  // rows stand in order, and a row's tokens in the order of its totals: how many of
-  // each row stand before a total is found by bisection
+  // Rows stand in order, and a row's tokens in the order of its totals: where there
+  // are many, how many of each row stand before a total is found by bisection.
   const int n = a.beams * width;
   const size_t out = static_cast<size_t>(group) * width;
   for (int i = tid; i < n; i += kJoinThreads) {
     const double total = totals[i];
     const int own = i / width;
     int rank = 0;
-    for (int b = 0; b < a.beams && rank < width; ++b) {
+    if (n <= 256) {
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) rank += totals[j] > total || (totals[j] == total && j < i) ? 1 : 0;
+    }
+    for (int b = n <= 256 ? a.beams : 0; b < a.beams && rank < width; ++b) {
       if (b == own) {
         rank += i % width;
         continue;
@@ -340,7 +368,7 @@ size_t beam_ws_bytes(int32_t rows, int32_t vocab, int32_t width) {
 }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s) {
-  const int each = each_of(a.rows, a.vocab), chunks = chunks_of(a.rows, a.vocab);
+  const int each = each_of(a.rows, a.vocab, a.width), chunks = chunks_of(a.rows, a.vocab, a.width);
   Stat* stats = static_cast<Stat*>(a.ws);
   Key* keys = reinterpret_cast<Key*>(stats + static_cast<size_t>(a.rows) * chunks);
   const dim3 grid(chunks, a.rows);
