@@ -190,8 +190,8 @@ __device__ __forceinline__ Places places(const ReorderArgs& a, int32_t head, int
   p.head = head;
   p.freed = freed;
   p.copies = copies;
-  p.taken = min(copies, freed + (a.num_free - p.head));
-  p.new_head = max(p.head + p.taken - freed, 0);
+  p.taken = min(copies, freed + min(a.num_free - p.head, copies));
+  p.new_head = max(p.head + (p.taken - freed), 0);
   p.back = min(max(freed - p.taken, 0), p.head);  // pages that return to the list
   return p;
 }
@@ -215,14 +215,14 @@ __device__ __forceinline__ void give(const ReorderArgs& a, const Scratch& w, con
   if (f < p.taken)
     place_copy(a, w, p, f, page);
   else if (f - p.taken < p.back)
-    a.free_pages[p.new_head + f - p.taken] = page;
+    a.free_pages[p.new_head + (f - p.taken)] = page;
 }
 
 // D: copies past the freed pages take the free list's, as far as there are any.
 // (Then no freed page goes back to the list that is read here.)
 __device__ void give_listed(const ReorderArgs& a, const Scratch& w, const Places& p) {
   for (int32_t c = p.freed + static_cast<int32_t>(threadIdx.x); c < p.copies; c += blockDim.x)
-    place_copy(a, w, p, c, c < p.taken ? a.free_pages[p.head + c - p.freed] : -1);
+    place_copy(a, w, p, c, c < p.taken ? a.free_pages[p.head + (c - p.freed)] : -1);
   if (threadIdx.x == 0) *a.free_head_out = p.new_head;
 }
 
