@@ -5,6 +5,10 @@
 // codes take u itself, without a rounding to 16 bits in between.
 //
 // WPR waves share a row; lane l of the row owns its 8-value chunks l, l + 64 WPR, ..
+//
+// Memory bounds it without codes (8384 rows of 5120 with a 32-bit residual: 515 MB in 92 us,
+// 5.6 TB/s); with codes the vector units are busy 72 % of the time (4192 rows of 2048: 15 us,
+// 60 MB), and weights and D^-1 come from the cache.
 #include "code_bits.h"
 #include "half_types.h"
 #include "token_internal.h"
@@ -174,16 +178,24 @@ hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// One 8-value chunk per lane, so that a row's loads are all in flight at once and no
+// lane does its divisions for more than it holds: a row of 1024 takes 2 waves (4096 rows
+// 8.5 us, with 4 waves 9.2), of 2048 4 waves (64 rows 3.2, with one wave 5.4), of 4096 8
+// waves (4096 rows 27.3, with 4 waves 29.1), of 8192 16 waves (4096 rows 50.2, with 4 waves
+// 55.9).  Between 4096 and 6144 values a third or more of 16 waves' lanes has none.  Few rows
+// (1 of 5120: 3.1, with 4 waves 4.5; 512 with codes 7.2 and 9.0) and rows without codes (4096
+// with a 32-bit residual 48.7 and 53.6) gain all the same; many with codes, whose two
+// divisions and two sums every wave repeats, are left at 4 waves (4096 rows 38.8, with 16
+// waves 47.1, with 8 43.4).
 hipError_t launch_add_rmsnorm(const NormArgs& a, hipStream_t s) {
   const int nch = a.K / 8;
   if (nch <= 64) return launch_rows<1, 1>(a, s);
-  switch ((nch + 255) / 256) {
-    case 1: return launch_rows<4, 1>(a, s);
-    case 2: return launch_rows<4, 2>(a, s);
-    case 3: return launch_rows<4, 3>(a, s);
-    case 4: return launch_rows<4, 4>(a, s);
-  }
-  return (nch + 1023) / 1024 <= 2 ? launch_rows<16, 2>(a, s) : launch_rows<16, 4>(a, s);
+  if (nch <= 128) return launch_rows<2, 1>(a, s);
+  if (nch <= 256) return launch_rows<4, 1>(a, s);
+  if (nch <= 512) return launch_rows<8, 1>(a, s);
+  if (nch <= 768 && a.qx != nullptr && a.M > 1024) return launch_rows<4, 3>(a, s);
+  if (nch <= 1024) return launch_rows<16, 1>(a, s);
+  return nch <= 2048 ? launch_rows<16, 2>(a, s) : launch_rows<16, 4>(a, s);
 }
 
 }  // namespace sq

@@ -67,7 +67,8 @@ def test_norm(M, K, dt, res, out):
         T.check(s, h, bh, DT[res], "sum")
 
 
-@pytest.mark.parametrize("M,K", [(1, 128), (5, 512), (4, 640), (9, 2048), (33, 5120), (2, 13824), (1, 32768), (1030, 256)])
+@pytest.mark.parametrize("M,K", [(1, 128), (5, 512), (4, 640), (9, 2048), (33, 5120), (2, 13824), (1, 32768), (1030, 256),
+                                 (3, 1024), (2, 4096), (4, 6144), (2, 8192), (1024, 5120), (1025, 4224), (1025, 6144), (1025, 6272)])
 @pytest.mark.parametrize("static,dinv,res,weight", [(False, True, "bf16", True), (True, True, None, True), (False, False, "f32", False),
                                                     (True, False, "f16", True)])
 def test_codes(M, K, static, dinv, res, weight):
