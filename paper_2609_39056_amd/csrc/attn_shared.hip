@@ -11,10 +11,15 @@
 // attention: scores as keys x queries, so that a lane has the probabilities that it
 // needs for the values, which it transposes in registers; nothing is passed
 // between lanes.
+//
+// Probabilities are in two 16-bit parts for 16-bit outputs (what is lost is under 2^-16
+// of a term, far below the output's rounding) and in three, all of fp32, for fp32
+// ones; those of a request's own tokens, which wait for memory, always in three.
 #include <type_traits>
 
 #include "attn_shared_split.h"
 #include "attn_tile.h"
+#include "gemm_frag.h"
 #include "token_internal.h"
 
 namespace sq {
@@ -147,14 +152,47 @@ __device__ bool find_chunk(const SharedArgs& a, const SharedSplit& sp, uint32_t 
 
 // Q tiles of query rows against one chunk: the prefix of a group (OWN false) or a
 // request's own tokens; probabilities as NP 16-bit parts.  The waves take the
-// chunk's tiles of tokens in turn, keys and values straight into registers, and are
-// joined through LDS.
+// chunk's tiles of tokens in turn, each for itself (no barrier), and are joined
+// through LDS.
+// Keys and values pass through LDS, a tile per wave, with direct loads whose lanes read
+// along the lines.  Straight into registers (as past a workgroup's share of LDS, at head
+// dimension 192) consecutive lanes read different rows of keys, four times the accesses
+// to the cache, which then bound the kernel: 64 rows of 5 heads on 8 by 8192 tokens took
+// 50.8 us (44.7), two groups of 16 rows on 8 by 32000 84 (60), 32 rows of 4 on 4 of 256 with
+// 400 tokens of their own 43 (37).  At 192 the LDS would leave one workgroup on a CU for two
+// (32 rows on 8 heads, 800 own tokens: 53.8 us, 40.3 in registers).
+template <int D>
+constexpr bool kThroughLds = D != 192;
+
 template <int D>
 struct Lds {
-  float values[kWaves][kQTile][D + 4], top[kWaves][kQTile], sum[kWaves][kQTile];
+  union {
+    uint8_t tile[kWaves][2][kThroughLds<D> ? kTile * 2 * D : 16];  // keys and values
+    struct {
+      float values[kWaves][kQTile][D + 4], top[kWaves][kQTile], sum[kWaves][kQTile];
+    };
+  };
   int32_t pages[static_cast<int>(kSharedMost) / kMinPage + 2];
 };
 static_assert(kAttnWhole <= kSharedMost, "one array holds the pages of either chunk");
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// dma<16> (gemm_frag.h) with an address of each lane's own.
+__device__ __forceinline__ void dma16_at(const void* p, uint32_t lds) {
+  const uint32_t m0v = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds)));
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(m0v), "v"(p) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// N dwords of LDS from a 4-byte boundary.
+template <int N>
+__device__ __forceinline__ void read_words(const uint8_t* p, uint32_t* w) {
+  typedef unsigned int vec __attribute__((ext_vector_type(N), aligned(N == 3 ? 4 : 4 * N)));
+  const vec r = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = r[i];
+}
 
 template <bool F16, int D, int Q, int NP, bool OWN>
 __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSplit& sp, uint32_t id, Lds<D>& lds) {
@@ -162,7 +200,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
   constexpr int KF = D / 32;  // fragments of a key row
   constexpr int E = D / 16, E0 = E < 8 ? E : 8, E1 = E - E0;  // a lane's dimensions of a value row
   constexpr int EW = E / 2;
-  constexpr bool kAhead = D < 256;
+  constexpr bool kStaged = kThroughLds<D>;
   constexpr int kRows = Q * kQTile;
   constexpr float kShift = F16 ? 11.0f : 0.0f;
   constexpr float kSlack = F16 ? 4.0f : 8.0f;
@@ -259,14 +297,17 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
   // values: tokens b + 16 i + 4 g + x, the lane's dimensions.  Where the tile lies
   // within one page of the range its address is the same for all lanes; tokens
   // outside [first, end) are not loaded: their lanes repeat the nearest row inside.
-  const int tiles = (end - begin + kTile - 1) / kTile;
   uint4 k[2][KF];
   uint32_t v[8][EW];
   auto inside = [&](int b) { return b >= first && b + kTile <= end; };
-  const bool one_page = shift >= 5;
-  auto tile_row = [&](int b) {
-    const int page = __builtin_amdgcn_readfirstlane(pages[(b >> shift) - page0]);
-    return ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + (b & mask);
+  const bool half_page = shift >= 4;
+  size_t half[2];  // rows of the cache where the halves of a tile begin
+  auto find_halves = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int page = __builtin_amdgcn_readfirstlane(page_of(b + 16 * i));
+      half[i] = ((static_cast<size_t>(max(page, 0)) * a.Hk + kvh) << shift) + ((b + 16 * i) & mask);
+    }
   };
   auto load_k_row = [&](int i, const uint16_t* p) {
 #pragma unroll
@@ -277,10 +318,9 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
     if constexpr (E1 > 0) load_words<E1 / 2, OWN>(p + 16 * E0 + E1 * c, w + E0 / 2);
   };
   auto load_k = [&](int b) {
-    if (one_page && inside(b)) {
-      const uint16_t* p = a.k + tile_row(b) * D;
+    if (half_page && inside(b)) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) load_k_row(i, p + static_cast<uint32_t>((16 * i + c) * D + 8 * g));
+      for (int i = 0; i < 2; ++i) load_k_row(i, a.k + half[i] * D + static_cast<uint32_t>(c * D + 8 * g));
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -290,10 +330,9 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
     }
   };
   auto load_v = [&](int b) {
-    if (one_page && inside(b)) {
-      const uint16_t* p = a.v + tile_row(b) * D;
+    if (half_page && inside(b)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) load_v_row(p + static_cast<uint32_t>((16 * (i / 4) + 4 * g + i % 4) * D), v[i]);
+      for (int i = 0; i < 8; ++i) load_v_row(a.v + half[i / 4] * D + static_cast<uint32_t>((4 * g + i % 4) * D), v[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -304,31 +343,92 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
       }
     }
   };
-  if (kAhead && wave < tiles) {
-    load_k(begin + wave * kTile);
-    load_v(begin + wave * kTile);
+  // Staged: 16-byte pieces go from memory into the wave's part of LDS, 64 to a load: piece
+  // 64 j + lane of 16 rows.  Those of a key row are turned by the row, so that the 16 rows that
+  // lanes read together lie in different banks.
+  constexpr int S = D / 8, kSame = D % 128 == 0 ? 1 : D == 96 ? 4 : 2;
+  constexpr int kLoads = 2 * KF;  // of 32 rows
+  auto turn = [&](int row) { return row / kSame; };
+  uint32_t k_from[KF], k_at[KF], v_from[KF];
+#pragma unroll
+  for (int j = 0; j < KF; ++j) {
+    const int row = (64 * j + lane) / S, piece = (64 * j + lane) % S - turn(row), at = 4 * j + g + turn(c);
+    k_from[j] = static_cast<uint32_t>(2 * D * row + 16 * (piece < 0 ? piece + S : piece));
+    v_from[j] = static_cast<uint32_t>(1024 * j + 16 * lane);
+    k_at[j] = static_cast<uint32_t>(2 * D * c + 16 * (at >= S ? at - S : at));
   }
-  for (int t = wave; t < tiles; t += W) {
-    const int b = begin + t * kTile;
-    if (!kAhead) {
-      load_k(b);
-      load_v(b);
+  const uint8_t *keys = lds.tile[wave][0], *values = lds.tile[wave][1];
+  // kLoads loads, after find_halves.  Where a half of the tile may lie in two pages or
+  // tokens of it outside [first, end), each lane has an address of its own, and those
+  // tokens repeat the nearest inside.
+  auto load_tile = [&](const uint16_t* cache, const uint32_t (&from)[KF], const uint8_t* to, int b) {
+    const uint32_t at = lds_offset(to);
+    if (half_page && inside(b)) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile before has been read
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < KF; ++j) dma<16>(cache + half[i] * D, from[j], at + 32 * D * i + 1024 * j);
+    } else {
+      auto token = [&](int i, int j) {
+        return max(first, min(b + 16 * i + static_cast<int>(from[j] / (2 * D)), end - 1));
+      };
+      int page[2][KF];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < KF; ++j) page[i][j] = page_of(token(i, j));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < KF; ++j)
+          dma16_at(cache + row_of(page[i][j], token(i, j)) * D + from[j] % (2 * D) / 2, at + 32 * D * i + 1024 * j);
     }
+  };
+  auto start_k = [&](int b) {
+    find_halves(b);
+    if constexpr (kStaged)
+      load_tile(a.k, k_from, keys, b);
+    else
+      load_k(b);
+  };
+  auto start_v = [&](int b) {
+    if constexpr (kStaged)
+      load_tile(a.v, v_from, values, b);
+    else
+      load_v(b);
+  };
+  if (begin + wave * kTile < end) {
+    start_k(begin + wave * kTile);
+    start_v(begin + wave * kTile);
+  }
+  for (int b = begin + wave * kTile; b < end; b += W * kTile) {
+    const int next = b + W * kTile;
+    const bool more = next < end;
+    if constexpr (kStaged) wait_vm<kLoads>();  // the keys; the values are behind them
     float f[Q][8];
 #pragma unroll
-    for (int y = 0; y < Q; ++y) {
+    for (int i = 0; i < 2; ++i) {
+      v4f s[Q];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        v4f s = v4f{0, 0, 0, 0};
+      for (int y = 0; y < Q; ++y) s[y] = v4f{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < KF; ++j) s = mfma<F16>(k[i][j], q[y][j], s);
+      for (int j = 0; j < KF; ++j) {
+        if constexpr (kStaged) k[i][j] = *reinterpret_cast<const uint4*>(keys + 32 * D * i + k_at[j]);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[x];
+        for (int y = 0; y < Q; ++y) s[y] = mfma<F16>(k[i][j], q[y][j], s[y]);
       }
+#pragma unroll
+      for (int y = 0; y < Q; ++y)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) f[y][4 * i + x] = s[y][x];
     }
-    if (kAhead && t + W < tiles) load_k(b + W * kTile);
+    if (more) start_k(next);
     float unit = scale;  // of f, in units of log 2
-    if (!(pages_ok && inside(b) && b + kTile <= least)) {
+    const bool masked = !(pages_ok && inside(b) && b + kTile <= least);
+    uint32_t dead = 0;
+    if (masked) {
       unit = 1.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -336,8 +436,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
         const bool live = (tok >= first) & (tok < end) & (page_of(tok) >= 0);
 #pragma unroll
         for (int y = 0; y < Q; ++y) f[y][i] = (live & (tok < limit[y])) ? f[y][i] * scale : -INFINITY;
-#pragma unroll
-        for (int w = 0; w < EW; ++w) v[i][w] = live ? v[i][w] : 0;
+        dead |= static_cast<uint32_t>(!live) << i;
       }
     }
     uint32_t p[Q][NP][4];
@@ -371,6 +470,24 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
         }
       }
     }
+    if constexpr (kStaged) {
+      if (more)
+        wait_vm<kLoads>();  // the values; the next keys are behind them
+      else
+        wait_vm<0>();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint8_t* row = values + 2 * D * (16 * (i / 4) + 4 * g + i % 4);
+        read_words<E0 / 2>(row + 2 * E0 * c, v[i]);
+        if constexpr (E1 > 0) read_words<E1 / 2>(row + 32 * E0 + 2 * E1 * c, v[i] + E0 / 2);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < EW; ++w) v[i][w] = dead >> i & 1 ? 0 : v[i][w];
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       uint4 vt;
@@ -385,7 +502,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
         for (int u = 0; u < NP; ++u)
           o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
     }
-    if (kAhead && t + W < tiles) load_v(b + W * kTile);
+    if (more) start_v(next);
   }
 
   // the waves' parts, a tile of rows at a time: column c, and the dimensions that lane 4 g + x loaded
@@ -396,7 +513,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
   for (int y = 0; y < Q; ++y) {
     if (kQTile * y >= rows) break;
     const float ls = quad_sum(l[y]);
-    if (y > 0) __syncthreads();
+    __syncthreads();
     if (g == 0) {
       s_m[wave][c] = m[y] - kShift;
       s_l[wave][c] = ls;

@@ -6,13 +6,12 @@
 // workgroups of the requests' own tokens, of at least 128 tokens.  Those are split as
 // in the paged attention.
 //
-// 384 workgroups (64 rows of 5 heads on 8 by 8192 tokens 50.6 us, 24 groups of 56 rows
-// by up to 4001 26.5, 64 rows on 8 by 32768 48.6, 16 groups of 20 rows on 8 by up to
-// 2048 25.4) are near the best everywhere: 256 take 49.0, 30.5, 54.2 and 27.1, 512 58.9,
-// 25.7, 56.0 and 27.4.  Past head dimension 128 registers leave one workgroup per CU:
-// 256 (32 rows of 8 heads of 256 by 4096 28.1 us, with 384 32.6).  Tiles of 64 rows were
-// slower in every form tried: sums in accumulation registers (the first of these 70 us),
-// keys and values through LDS for four waves of 16 or 32 rows (56 and 53).
+// Workgroups wanted, 384 up to head dimension 64, where a CU holds three of them, and 256
+// past it: with 256 and 384, 24 groups of 56 rows of 64 by up to 4001 take 27.9 and 24.2 us;
+// of 128, 64 rows of 5 heads on 8 by 8192 44.7 and 45.3, two groups of 16 rows on 8 by 32000
+// 60.3 and 65.6, and 8 groups of 32 rows of 96 on 4 by 4096 22.4 and 26.7 (512: 24.6, 50.5, 68.7
+// and 30.3).  Tiles of 64 rows were slower in every form tried: sums in accumulation registers
+// (70 us for the second), keys and values through LDS for four waves together (56 and 53).
 #pragma once
 
 #include <stdint.h>
@@ -23,7 +22,7 @@
 
 namespace sq {
 
-constexpr int64_t kSharedWanted = 384;      // workgroups that chunks are made for
+constexpr int64_t kSharedWanted = 384;      // workgroups that chunks are made for, at most
 constexpr int64_t kSharedLeast = 128;       // tokens of a chunk, unless the prefix is shorter
 constexpr int64_t kSharedMost = 8192;
 constexpr int32_t kSharedRows = 32;         // the most query rows of a workgroup
@@ -59,7 +58,7 @@ inline SharedSplit shared_split(int32_t R, int32_t groups, int32_t Hq, int32_t H
   const int64_t rows = static_cast<int64_t>(R) * each;
   s.slots = static_cast<int32_t>(rows / s.rows + groups);
   const int64_t busy = Hk * std::max<int64_t>(std::max(1, groups), (rows + s.rows - 1) / s.rows);
-  const int64_t want = std::max<int64_t>(1, (D <= 128 ? kSharedWanted : 256) / busy);
+  const int64_t want = std::max<int64_t>(1, (D <= 64 ? kSharedWanted : 256) / busy);
   const int64_t even = ((max_shared + want - 1) / want + 31) / 32 * 32;
   const int64_t chunk = std::min(kSharedMost, std::max(kSharedLeast, even));
   s.chunk = static_cast<int32_t>(chunk);
