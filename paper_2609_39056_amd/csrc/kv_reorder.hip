@@ -13,11 +13,12 @@
 //   C  freed pages per dropped row
 //   D  their places in the list of freed pages (a sum over the rows before), of
 //      which the first go to the copies and the rest back to the free list
-// Large tables take a launch per phase, a wave per row (1024 rows of up to 290 pages: 25 us).
-// Small ones take one workgroup with barriers between the phases, whose threads
-// keep their entries in registers and whose scratch is in LDS, so that only the
-// lengths, the entries and the last pages are dependent loads (64 rows of 80: 11.3 us,
-// in four launches 15.7).
+// What bounds it is dependent loads and launches, not data.  Large tables take a launch
+// per phase, a wave per row (1024 rows of up to 290 pages: 25 us, of which the phases take
+// 7.0, 6.4, 6.3 and 6.4).  Small ones take one workgroup with barriers between the phases,
+// which has the entries and the scratch in LDS, so that only the lengths, the entries and
+// the last pages are dependent loads (64 rows of up to 142 pages: 11.3 us, in four
+// launches 15.7).
 #include <algorithm>
 
 #include "token_internal.h"
