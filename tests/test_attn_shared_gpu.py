@@ -178,7 +178,8 @@ def test_groups(Hq, Hk, D, dt, out):
     check(case(sizes, shared, kv_len, Hq, Hk, D, 16, dt), out)
 
 
-@pytest.mark.parametrize("page,Hq,Hk,D", [(8, 4, 2, 64), (128, 8, 1, 128), (1024, 2, 2, 96)])
+@pytest.mark.parametrize("page,Hq,Hk,D", [(8, 4, 2, 64), (128, 8, 1, 128), (1024, 2, 2, 96), (8, 6, 1, 128), (8, 3, 1, 96), (8, 4, 1, 192),
+                                          (8, 4, 1, 256), (16, 6, 1, 96), (64, 10, 2, 256), (32, 5, 1, 192), (16, 12, 1, 64)])
 def test_one_long_prefix(page, Hq, Hk, D):
     # many chunks, one group, requests whose own part is empty, one token, more than a chunk
     s = 5000 if page < 1024 else 4096
@@ -353,3 +354,45 @@ def test_graph_replays_with_other_lengths():
             call(eager, ws2)
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(o, eager)
+
+
+def test_cache_offsets_past_32_bits():
+    # the pages of a small case at both ends of a cache whose byte and element offsets both pass 2^32
+    c = case([5, 3], [700, 64], [720, 701, 900, 700, 640, 64, 65, 300], 4, 2, 128, 64, "bf16", seed=3)
+    o, lse = run(c, "f32")
+    n, many = c["k"].shape[0], 140000
+    ids = torch.cat([torch.arange(n // 2), torch.arange(many - (n - n // 2), many)])
+    big = {}
+    for x in "kv":
+        big[x] = torch.empty((many, *c[x].shape[1:]), dtype=torch.bfloat16, device="cuda")
+        big[x][ids.cuda()] = c[x].cuda()
+    assert big["k"].numel() > 1 << 31 and big["k"].nbytes > 1 << 32
+    kv = B.KVCache(big["k"], big["v"])
+    table = torch.where(c["table"] < 0, c["table"], ids.to(torch.int32)[c["table"].long().clamp(min=0)]).cuda()
+    R, Hq, D = c["q"].shape
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    B.sq_attn_shared(c["q"].cuda(), kv, table, i32(c["kv_len"]), i32(c["start"]), i32(c["shared"]), 700, 900, c["scale"], o2,
+                     B.SQ_OUT_F32, lse2, B.alloc_attn_shared_workspace(R, 2, Hq, kv, 700, 900))
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_two_graphs_share_a_workspace():
+    cases = [case([4, 3], [300, 77], [400] * 4 + [150] * 3, 8, 2, 128, 16, "bf16", seed=1),
+             case([40], [1500], [1500 + 7 * r for r in range(40)], 8, 2, 128, 64, "bf16", seed=2)]
+    want = [run(c, "bf16")[0] for c in cases]
+    kvs = [B.KVCache(c["k"].cuda(), c["v"].cuda()) for c in cases]
+    ws = B.alloc_attn_shared_workspace(40, 2, 8, kvs[1], 1500, 2000)
+    graphs, outs, keep = [], [], []
+    for c, kv, w in zip(cases, kvs, want):
+        o = torch.zeros_like(w)
+        args = (c["q"].cuda(), kv, c["table"].cuda(), i32(c["kv_len"]), i32(c["start"]), i32(c["shared"]), max(c["shared"]),
+                max(c["kv_len"]), c["scale"], o, B.SQ_OUT_BF16, None, ws)
+        B.sq_attn_shared(*args)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.sq_attn_shared(*args)
+        graphs.append(graph), outs.append(o), keep.append(args)
+    for i in (0, 1, 0, 0, 1, 1, 0):
+        outs[i].zero_()
+        graphs[i].replay()
+        assert torch.equal(outs[i], want[i])

@@ -346,3 +346,51 @@ def test_copy_nothing():
     B.sq_kv_copy_pages([], i32([0]), i32([1]), None)
     B.sq_kv_copy_pages([kv], i32([0, 1]), i32([2, 3]), i32([0, -1]))
     assert torch.equal(k, was)
+
+
+def test_copy_past_32_bits():
+    # element offsets beyond 2^31 and byte offsets beyond 2^32, both ways
+    n, shape = 140000, (2, 64, 128)
+    k, v = (torch.empty((n, *shape), dtype=torch.float16, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 31 and k.nbytes > 1 << 32
+    g = torch.Generator().manual_seed(4)
+    src, dst, rows = [n - 1, 3, n - 5], [2, n - 2, n - 9], [64, 17, 33]
+    for t in (k, v):
+        for p in src:
+            t[p] = torch.randn(shape, generator=g).half().cuda()
+        for p in dst:
+            t[p] = 7.0
+    want = [[torch.cat([t[s][:, :r], t[d][:, r:]], 1) for s, d, r in zip(src, dst, rows)] for t in (k, v)]
+    B.sq_kv_copy_pages([B.KVCache(k, v)], i32(src), i32(dst), i32(rows))
+    for t, w in zip((k, v), want):
+        assert all(torch.equal(t[d], x) for d, x in zip(dst, w))
+
+
+def test_reorder_two_graphs_share_a_workspace():
+    # one of a small table (one launch), one of a large one (four)
+    rng = np.random.default_rng(8)
+    calls = []
+    for n, most, num_pages in ((12, 5, 64), (1500, 40, 40000)):
+        table = rng.integers(0, num_pages, (n, most)).tolist()
+        kv_len, parent = rng.integers(0, most * 16 + 1, n).tolist(), rng.integers(0, n, n).tolist()
+        calls.append(dict(parent=i32(parent), kv_len=i32(kv_len), table=i32(table), free0=i32(list(range(num_pages))), num=num_pages,
+                          head=i32([num_pages // 2]), out=[torch.full((n, most), -9, dtype=torch.int32, device="cuda")] +
+                          [i32([0] * n) for _ in range(4)] + [i32([0])]))
+    shared = B.alloc_reorder_workspace(1500, 40000)
+
+    def call(c, ws):
+        o = c["out"]
+        B.sq_kv_reorder(c["parent"], c["kv_len"], 16, c["num"], c["free"], c["head"], c["table"], o[0], o[1], o[2], o[3], o[4], o[5], ws)
+
+    for c in calls:
+        c["free"] = c["free0"].clone()
+        call(c, torch.full_like(B.alloc_reorder_workspace(len(c["parent"]), c["num"]), 0x5A))
+        c["want"] = [t.clone() for t in c["out"] + [c["free"]]]
+        c["graph"] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(c["graph"]):
+            call(c, shared)
+    for i in (0, 1, 1, 0, 1, 0):
+        c = calls[i]
+        c["free"].copy_(c["free0"])
+        c["graph"].replay()
+        assert all(torch.equal(a, b) for a, b in zip(c["out"] + [c["free"]], c["want"]))
