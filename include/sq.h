@@ -607,8 +607,8 @@ sq_status sq_linear_w4a16(const uint16_t* x, int32_t M, const float* dinv, const
  * 8 <= K <= 32768, K % 8 == 0, with act K % 128 == 0; strides are multiples of
  * 8 and at least K; eps >= 0, finite.  At least one output is required.  Tensors
  * and weights 16-byte aligned, act_scale 4.  `sum` may be the residual, `sum` or
- * y may be x (of the same type and stride); other outputs must not overlap
- * inputs.  Inputs must be finite, and so must the sum of a row's h^2. */
+ * y may be x, of the same type and stride (else SQ_ERR_UNSUPPORTED); other outputs
+ * must not overlap inputs.  Inputs must be finite, and so must the sum of a row's h^2. */
 sq_status sq_add_rmsnorm(const void* x, int64_t x_stride, int32_t x_dtype, const void* residual, int64_t residual_stride,
                          int32_t residual_dtype, const float* weight, float eps, int32_t M, int32_t K, void* sum,
                          int64_t sum_stride, void* y, int32_t y_dtype, const sq_act_params* act, int8_t* qx,

@@ -1038,6 +1038,14 @@ sq_status sq_add_rmsnorm(const void* x, int64_t x_stride, int32_t x_dtype, const
   if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(sum, 16) || !aligned(y, 16) ||
       (act != nullptr && (!aligned(qx, 16) || !aligned(act_scale, 4))))
     return SQ_ERR_ALIGN;
+  // an output takes an input's place element by element, or rows would overtake each other
+  auto moved = [&](const void* in, int32_t in_dtype, int64_t in_stride, const void* out, int32_t dtype, int64_t stride) {
+    return out != nullptr && in == out && (in_dtype != dtype || (M > 1 && in_stride != stride));
+  };
+  if (moved(x, x_dtype, x_stride, sum, residual_dtype, sum_stride) || moved(x, x_dtype, x_stride, y, y_dtype, K) ||
+      moved(residual, residual_dtype, residual_stride, sum, residual_dtype, sum_stride) ||
+      moved(residual, residual_dtype, residual_stride, y, y_dtype, K))
+    return SQ_ERR_UNSUPPORTED;
   NormArgs a{};
   a.x = x;
   a.residual = residual;
@@ -1115,7 +1123,8 @@ sq_status sq_attn_shared(const void* q, int64_t q_stride, int32_t num_requests, 
   if (st != SQ_OK) return st;
   if (!valid_out(out_dtype) || !std::isfinite(scale)) return SQ_ERR_UNSUPPORTED;
   const int64_t most = static_cast<int64_t>(max_pages) * kv->page_size;
-  if (!valid_shared_sizes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len) || max_pages < 1 || most >= kIndexEnd || max_shared_len > most || max_own_len > most)
+  if (!valid_shared_sizes(num_requests, num_groups, q_heads, kv, max_shared_len, max_own_len) || max_pages < 1 ||
+      most >= kIndexEnd || max_shared_len > most || max_own_len > most)
     return SQ_ERR_SHAPE;
   if (num_requests == 0) return SQ_OK;
   if (q == nullptr || table == nullptr || kv_len == nullptr || out == nullptr || workspace == nullptr ||

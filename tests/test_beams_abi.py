@@ -32,6 +32,8 @@ def norm(L, a=False, **kw):  # noqa: F811
     (dict(xs=260), SHAPE), (dict(rs=-256), SHAPE), (dict(ss=128), SHAPE), (dict(a=dict(step=9)), SHAPE), (dict(x=A + 8), ALIGN),
     (dict(res=A + 2), ALIGN), (dict(w=A + 4), ALIGN), (dict(sum=A + 8), ALIGN), (dict(y=A + 8), ALIGN), (dict(a={}, qx=A + 8), ALIGN),
     (dict(a={}, r=A + 2), ALIGN), (dict(a=dict(dinv=A + 4)), ALIGN), (dict(M=0), OK), (dict(M=0, x=None, y=None, sum=None), OK),
+    (dict(rs=512), UNSUP), (dict(ss=512), UNSUP), (dict(y=None, x=A + 64, ss=264), UNSUP), (dict(sum=None, xs=512), UNSUP),
+    (dict(sum=None, res=A + 64, yd=0), UNSUP), (dict(res=A + 64, rd=0, y=None), UNSUP), (dict(sum=None, x=A + 64, yd=2), UNSUP),
 ])
 def test_norm_rejects(L, kw, code):  # noqa: F811
     assert norm(L, **kw) == code
