@@ -176,25 +176,6 @@ struct Lds {
 };
 static_assert(kAttnWhole <= kSharedMost, "one array holds the pages of either chunk");
 
-// Direct loads of 16 bytes a lane to LDS, lane i's at `lds` + 16 i (the same in all lanes),
-// from an offset per lane to one base, or from an address per lane.  M0 wants a wait state
-// before it is used.  The kernel counts and waits for them itself (wait_vm).
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ uint32_t same(uint32_t v) {
-  return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
-}
-__device__ __forceinline__ void load_to_lds(const uint16_t* base, uint32_t offset, uint32_t lds) {
-  const uint64_t b = reinterpret_cast<uint64_t>(base);
-  const uint64_t from = static_cast<uint64_t>(same(static_cast<uint32_t>(b >> 32))) << 32 | same(static_cast<uint32_t>(b));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(same(lds)), "v"(offset), "s"(from)
-               : "memory", "m0");
-}
-__device__ __forceinline__ void load_to_lds(const uint16_t* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(same(lds)), "v"(p) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
 // N dwords of LDS from a 4-byte boundary.
 template <int N>
 __device__ __forceinline__ void read_words(const uint8_t* p, uint32_t* w) {
@@ -378,7 +359,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < KF; ++j) load_to_lds(cache + half[i] * D, from[j], at + 32 * D * i + 1024 * j);
+        for (int j = 0; j < KF; ++j) dma<16>(cache + half[i] * D, from[j], at + 32 * D * i + 1024 * j);
     } else {
       auto token = [&](int i, int j) {
         return max(first, min(b + 16 * i + static_cast<int>(from[j] / (2 * D)), end - 1));
@@ -393,7 +374,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < KF; ++j)
-          load_to_lds(cache + row_of(page[i][j], token(i, j)) * D + from[j] % (2 * D) / 2, at + 32 * D * i + 1024 * j);
+          dma16_lanes(cache + row_of(page[i][j], token(i, j)) * D + from[j] % (2 * D) / 2, at + 32 * D * i + 1024 * j);
     }
   };
   auto start_k = [&](int b) {
