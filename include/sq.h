@@ -666,10 +666,8 @@ size_t sq_attn_shared_workspace_bytes(int32_t num_requests, int32_t num_groups, 
  * most of them; tokens from p on are each request's own.  A request attends
  * kv_len[r] tokens, also where that is less than p, and at most p + max_own_len;
  * one of no group has p = 0.  Everything else (scores, what empty rows, NaN and
- * infinities give, fp32 sums, cache rows that are not attended, the types and sizes)
- * is as in sq_attn_paged; probabilities of the shared tokens enter their product
- * with 16 (bf16) or 22 (f16) bits for 16-bit outputs, with all 24 for fp32 ones and
- * for the requests' own tokens.
+ * infinities give, fp32 sums and probabilities, cache rows that are not attended, the
+ * types and sizes) is as in sq_attn_paged.
  *   group_start  int32 [num_groups + 1], not falling, in [0, num_requests] (clamped;
  *                requests of groups that overlap get unspecified results)
  *   shared_len   int32 [num_groups]; both may be NULL with num_groups 0

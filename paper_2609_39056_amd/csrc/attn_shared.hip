@@ -12,9 +12,10 @@
 // needs for the values, which it transposes in registers; nothing is passed
 // between lanes.
 //
-// Probabilities are in two 16-bit parts for 16-bit outputs (what is lost is under 2^-16
-// of a term, far below the output's rounding) and in three, all of fp32, for fp32
-// ones; those of a request's own tokens, which wait for memory, always in three.
+// Probabilities enter their product as three 16-bit parts, all 24 bits of fp32, for every
+// output type: with two of bf16 a sum that cancels was off by twice the bound of fp32
+// probabilities.  The third costs nothing where memory bounds, and up to 8 % where the
+// arithmetic does (64 rows of 5 heads on 8 by 8192 tokens: 45.7 us with two, 49 to 50).
 #include <type_traits>
 
 #include "attn_shared_split.h"
@@ -27,6 +28,7 @@ namespace {
 
 constexpr int kTile = kAttnTile, kQTile = kAttnQTile;
 constexpr int kMinPage = 8;
+constexpr int kParts = 3;  // 16-bit parts of a probability
 constexpr int kWaves = 4;
 
 // The parts of the prefix and of the requests' own tokens, [row][chunk] of each
@@ -151,9 +153,8 @@ __device__ bool find_chunk(const SharedArgs& a, const SharedSplit& sp, uint32_t 
 }
 
 // Q tiles of query rows against one chunk: the prefix of a group (OWN false) or a
-// request's own tokens; probabilities as NP 16-bit parts.  The waves take the
-// chunk's tiles of tokens in turn, each for itself (no barrier), and are joined
-// through LDS.
+// request's own tokens.  The waves take the chunk's tiles of tokens in turn, each for
+// itself (no barrier), and are joined through LDS.
 // Keys and values pass through LDS, a tile per wave, with direct loads whose lanes read
 // along the lines.  Straight into registers (as past a workgroup's share of LDS, at head
 // dimension 192) consecutive lanes read different rows of keys, four times the accesses
@@ -185,7 +186,7 @@ __device__ __forceinline__ void read_words(const uint8_t* p, uint32_t* w) {
   for (int i = 0; i < N; ++i) w[i] = r[i];
 }
 
-template <bool F16, int D, int Q, int NP, bool OWN>
+template <bool F16, int D, int Q, bool OWN>
 __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSplit& sp, uint32_t id, Lds<D>& lds) {
   constexpr int W = kWaves;
   constexpr int KF = D / 32;  // fragments of a key row
@@ -430,7 +431,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
         dead |= static_cast<uint32_t>(!live) << i;
       }
     }
-    uint32_t p[Q][NP][4];
+    uint32_t p[Q][kParts][4];
 #pragma unroll
     for (int y = 0; y < Q; ++y) {
       float top = f[y][0];
@@ -452,9 +453,9 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
         float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(f[y][i + 1], unit, from));
         l[y] += x0 + x1;
 #pragma unroll
-        for (int u = 0; u < NP; ++u) {
+        for (int u = 0; u < kParts; ++u) {
           p[y][u][i / 2] = to_half2<F16>(x0, x1);
-          if (u + 1 < NP) {
+          if (u + 1 < kParts) {
             x0 -= half_lo<F16>(p[y][u][i / 2]);
             x1 -= half_hi<F16>(p[y][u][i / 2]);
           }
@@ -490,7 +491,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 #pragma unroll
       for (int y = 0; y < Q; ++y)
 #pragma unroll
-        for (int u = 0; u < NP; ++u)
+        for (int u = 0; u < kParts; ++u)
           o[y][e] = mfma<F16>(vt, make_uint4(p[y][u][0], p[y][u][1], p[y][u][2], p[y][u][3]), o[y][e]);
     }
     if (more) start_v(next);
@@ -544,14 +545,14 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
 
 // The prefixes' workgroups, ROWS query rows each, then those of the requests' own
 // tokens: the former compute, the latter wait for memory, and run beside them.
-template <bool F16, int D, int ROWS, int NP>
+template <bool F16, int D, int ROWS>
 __global__ __launch_bounds__(64 * kWaves, D <= 128 ? 2 : 1) void shared_kernel(SharedArgs a, SharedSplit sp) {
   __shared__ Lds<D> lds;
   const uint32_t id = static_cast<uint32_t>(flat_wg());
   if (id < sp.prefix_wgs)
-    take_tokens<F16, D, ROWS / kQTile, NP, false>(a, sp, id, lds);
+    take_tokens<F16, D, ROWS / kQTile, false>(a, sp, id, lds);
   else if (id - sp.prefix_wgs < sp.own_wgs)
-    take_tokens<F16, D, 1, 3, true>(a, sp, id - sp.prefix_wgs, lds);
+    take_tokens<F16, D, 1, true>(a, sp, id - sp.prefix_wgs, lds);
 }
 
 // Joins the parts of a query head: a thread takes four dimensions.
@@ -606,19 +607,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a, SharedSp
   if (d4 == 0 && a.lse != nullptr) a.lse[row] = empty ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * kLn2;
 }
 
-template <bool F16, int D, int NP>
-void launch_rows(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
-  const dim3 grid = wg_grid(static_cast<size_t>(sp.prefix_wgs) + sp.own_wgs);
-  if (sp.rows == 16) {
-    shared_kernel<F16, D, 16, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
-  } else if constexpr (D <= 192) {
-    shared_kernel<F16, D, 32, NP><<<grid, 64 * kWaves, 0, s>>>(a, sp);
-  }
-}
-
 template <bool F16, int D>
 void launch_dim(const SharedArgs& a, const SharedSplit& sp, hipStream_t s) {
-  a.out_dtype == SQ_OUT_F32 ? launch_rows<F16, D, 3>(a, sp, s) : launch_rows<F16, D, 2>(a, sp, s);
+  const dim3 grid = wg_grid(static_cast<size_t>(sp.prefix_wgs) + sp.own_wgs);
+  if (sp.rows == 16) {
+    shared_kernel<F16, D, 16><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  } else if constexpr (D <= 192) {
+    shared_kernel<F16, D, 32><<<grid, 64 * kWaves, 0, s>>>(a, sp);
+  }
 }
 
 template <bool F16>
