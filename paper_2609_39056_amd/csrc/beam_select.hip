@@ -15,8 +15,7 @@
 // Reading bounds the chunks where there is much to read, with the vector units at 57 %
 // (128 rows of 131071 bf16, 34 MB: 13 us, and 7 for the join of 16 workgroups); else the
 // two launches do (4 rows of 8192: 3.9 and 4.5 us).
-#include <algorithm>
-
+#include "beam_split.h"
 #include "half_types.h"
 #include "token_internal.h"
 
@@ -25,7 +24,7 @@ namespace {
 
 typedef unsigned long long Key;  // 0: none
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = kBeamThreads, kWaves = kThreads / 64;
 constexpr int kMaxWidth = 64;
 constexpr int kList = 1024;  // values that a workgroup orders; more only where very many are equal
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -36,6 +35,7 @@ struct Stat {
   float top;
   int32_t unused;
 };
+static_assert(sizeof(Stat) + sizeof(Key) == beam_chunk_bytes(1), "what the workspace holds of a chunk");
 
 // Bits whose order is that of the values (-0 counts as 0).
 __device__ __forceinline__ uint32_t order_of(float v) {
@@ -198,26 +198,8 @@ __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a, Key* k
 // One workgroup per group of beams: a wave per row joins its chunks, then the
 // rows' best are ordered.
 constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
-constexpr int kLeastEach = 8, kMostEach = 32;
 constexpr int kJoinList = 512;                                   // keys of a wave that are ordered together
-constexpr int kLists = (1 << 20) / (kThreads * kMostEach) / 64;  // chunks of a lane, of the largest vocabulary
-
-// Values of a thread.  Short chunks fill the chip where there is little to read, but
-// leave more keys to join: 2048 tokens up to 1024 chunks, 4096 up to 8192, and longer
-// ones where a row would leave more than 256 keys (128 rows of 131071, 8 each: 24.1,
-// 20.9 and 20.0 us with 2048, 4096 and 8192 tokens; 8 rows, 16 each: 24.6, 19.3, 15.9;
-// 64 rows of 32000, 4 each: 10.1, 10.1, 10.9).
-int each_of(int32_t rows, int32_t vocab, int32_t width) {
-  auto chunks = [&](int each) { return static_cast<int64_t>((vocab + kThreads * each - 1) / (kThreads * each)); };
-  int each = vocab > (1 << 18) ? 32 : kLeastEach;
-  if (each == 8 && (rows * chunks(8) > 1024 || chunks(8) * width > 256)) each = 16;
-  if (each == 16 && (rows * chunks(8) > 8192 || chunks(16) * width > 256)) each = 32;
-  return each;
-}
-int chunks_of(int32_t rows, int32_t vocab, int32_t width) {
-  const int tokens = kThreads * each_of(rows, vocab, width);
-  return (vocab + tokens - 1) / tokens;
-}
+constexpr int kLists = (1 << 20) / (kThreads * kBeamMostEach) / 64;  // chunks of a lane, of the largest vocabulary
 
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, const Key* keys, const Stat* stats, int chunks) {
   extern __shared__ double totals[];  // [beams][width], then their tokens
@@ -363,16 +345,12 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a, con
 
 }  // namespace
 
-// For every call with as many rows and tokens or fewer: the smallest chunks of
-// at most 8192 in all, or 4096 tokens each.
 size_t beam_ws_bytes(int32_t rows, int32_t vocab, int32_t width) {
-  const size_t r = rows;
-  const size_t most = std::max(r * ((vocab + 4095) / 4096), std::min<size_t>(8192 + r, r * ((vocab + 2047) / 2048)));
-  return most * (sizeof(Stat) + width * sizeof(Key));
+  return static_cast<size_t>(beam_most_chunks(rows, vocab)) * beam_chunk_bytes(width);
 }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s) {
-  const int each = each_of(a.rows, a.vocab, a.width), chunks = chunks_of(a.rows, a.vocab, a.width);
+  const int each = beam_each(a.rows, a.vocab, a.width), chunks = beam_chunks(a.vocab, each);
   Stat* stats = static_cast<Stat*>(a.ws);
   Key* keys = reinterpret_cast<Key*>(stats + static_cast<size_t>(a.rows) * chunks);
   const dim3 grid(chunks, a.rows);
