@@ -182,7 +182,7 @@ hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
 // lane does its divisions for more than it holds: a row of 1024 takes 2 waves (4096 rows
 // 8.5 us, with 4 waves 9.2), of 2048 4 waves (64 rows 3.2, with one wave 5.4), of 4096 8
 // waves (4096 rows 27.3, with 4 waves 29.1), of 8192 16 waves (4096 rows 50.2, with 4 waves
-// 55.9).  Between 4096 and 6144 values a third or more of 16 waves' lanes has none.  Few rows
+// 55.9).  Between 4096 and 6144 values half to a quarter of 16 waves' lanes has none.  Few rows
 // (1 of 5120: 3.1, with 4 waves 4.5; 512 with codes 7.2 and 9.0) and rows without codes (4096
 // with a 32-bit residual 48.7 and 53.6) gain all the same; many with codes, whose two
 // divisions and two sums every wave repeats, are left at 4 waves (4096 rows 38.8, with 16

@@ -158,10 +158,10 @@ __device__ bool find_chunk(const SharedArgs& a, const SharedSplit& sp, uint32_t 
 // Keys and values pass through LDS, a tile per wave, with direct loads whose lanes read
 // along the lines.  Straight into registers (as past a workgroup's share of LDS, at head
 // dimension 192) consecutive lanes read different rows of keys, four times the accesses
-// to the cache, which then bound the kernel: 64 rows of 5 heads on 8 by 8192 tokens took
-// 50.8 us (44.7), two groups of 16 rows on 8 by 32000 84 (60), 32 rows of 4 on 4 of 256 with
-// 400 tokens of their own 43 (37).  At 192 the LDS would leave one workgroup on a CU for two
-// (32 rows on 8 heads, 800 own tokens: 53.8 us, 40.3 in registers).
+// to the cache: 64 rows of 5 heads on 8 by 8192 tokens took 51.3 us (50.4), two groups of 16
+// rows on 8 by 32000 68.5 (61.0), 8 groups of 32 rows of 64 on 8 with 2000 tokens of their own
+// 60.7 (47.1), 32 rows of 4 on 4 of 256 with 400 own 41.5 (38.3).  At 192 the LDS would leave
+// one workgroup on a CU for two (32 rows on 8 heads, 800 own tokens: 53.6 us, 40.5 in registers).
 template <int D>
 constexpr bool kThroughLds = D != 192;
 

@@ -7,11 +7,12 @@
 // in the paged attention.
 //
 // Workgroups wanted, 384 up to head dimension 64, where a CU holds three of them, and 256
-// past it: with 256 and 384, 24 groups of 56 rows of 64 by up to 4001 take 27.9 and 24.2 us;
-// of 128, 64 rows of 5 heads on 8 by 8192 44.7 and 45.3, two groups of 16 rows on 8 by 32000
-// 60.3 and 65.6, and 8 groups of 32 rows of 96 on 4 by 4096 22.4 and 26.7 (512: 24.6, 50.5, 68.7
-// and 30.3).  Tiles of 64 rows were slower in every form tried: sums in accumulation registers
-// (70 us for the second), keys and values through LDS for four waves together (56 and 53).
+// past it: with 256 and 384, 24 groups of 56 rows of 64 by up to 4001 take 28.2 and 24.5 us;
+// of 128, 64 rows of 5 heads on 8 by 8192 50.4 to 51.0 and 49.5, two groups of 16 rows on 8 by
+// 32000 61.0 and 66.4, and 8 groups of 32 rows of 96 on 4 by 4096 22.7 and 27.3 (512: 24.8, 54.1,
+// 68.9 and 30.7).  Tiles of 64 rows were slower in every form tried, then with two parts of a
+// probability and 45 us for the second case: sums in accumulation registers (70 us), keys and
+// values through LDS for four waves together (56 and 53).
 #pragma once
 
 #include <stdint.h>

@@ -12,7 +12,7 @@
 // of each row of a group, in the same way, and the rows.  Totals are fp64: beams
 // of one prompt lie next to each other.
 //
-// Reading bounds the chunks where there is much to read, with the vector units at 57 %
+// Reading bounds the chunks where there is much to read, with the vector units at 55 %
 // (128 rows of 131071 bf16, 34 MB: 13 us, and 7 for the join of 16 workgroups); else the
 // two launches do (4 rows of 8192: 3.9 and 4.5 us).
 #include "beam_split.h"

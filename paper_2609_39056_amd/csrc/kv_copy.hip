@@ -3,8 +3,8 @@
 // of its heads are runs of rows * head_dim values; a workgroup takes a share of
 // one page of one tensor, in 16-byte pieces.
 //
-// Memory bounds it (128 copies in 28 layers, 846 MB read and written: 179 to 191 us, 4.4 to
-// 4.7 TB/s, as fast as a plain copy of 4 GiB), and at little data the launch (48 copies in
+// Memory bounds it (128 copies in 28 layers, 846 MB read and written: 175 to 191 us, 4.4 to
+// 4.8 TB/s, as fast as a plain copy of 4 GiB), and at little data the launch (48 copies in
 // one layer: 3.0 us).  Four pieces of a thread in flight: with 1, 2, 4 and 8 the former
 // takes 219, 188, 187 and 182 us, the latter 3.4, 3.7, 3.2 and 3.7, 64 copies of small pages
 // in 28 layers 30.5, 24.5, 23.2 and 22.9.  Loads and stores past the caches gained nothing.
