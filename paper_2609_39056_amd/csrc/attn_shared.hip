@@ -359,8 +359,7 @@ __device__ __forceinline__ void take_tokens(const SharedArgs& a, const SharedSpl
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile before has been read
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < KF; ++j) dma<16>(cache + half[i] * D, from[j], at + 32 * D * i + 1024 * j);
+        dma_run(cache + half[i] * D, from, at + 32 * D * i);
     } else {
       auto token = [&](int i, int j) {
         return max(first, min(b + 16 * i + static_cast<int>(from[j] / (2 * D)), end - 1));

@@ -131,10 +131,8 @@ __global__ __launch_bounds__(256, (Sk<ABITS, QX, BM, BN>::WGS_PER_CU)) void gemm
   const uint16_t* sig = static_cast<const uint16_t*>(a.act_scale) + static_cast<size_t>(m0) * (K / kA4Group);
   auto issue = [&](int kt, int slot) {
     const uint32_t st = ring0 + slot * L::SLOT;
-#pragma unroll
-    for (int i = 0; i < L::A / 1024; ++i) dma<16>(qx + kt * (arow / nkt), voffA[i], st + i * 1024);
-#pragma unroll
-    for (int i = 0; i < L::B / 1024; ++i) dma<16>(qw + kt * (KT / 2), voffB[i], st + L::B_OFF + i * 1024);
+    dma_run(qx + kt * (arow / nkt), voffA, st);
+    dma_run(qw + kt * (KT / 2), voffB, st + L::B_OFF);
     if constexpr (ABITS == 4) dma<4>(sig + 2 * kt, voffS, st + L::S_OFF);  // the stage's two groups
     // group-major steps of the stage's weight group
     dma<4>(a.w_scale + static_cast<size_t>((kt * KT) / a.w_group) * N + n0, voffW, st + L::W_OFF);

@@ -243,7 +243,7 @@ __global__ __launch_bounds__(1024) void linear_staged_kernel(LinearArgs a) {
 // of four waves, two to a CU (36.0; unscaled 22.5, eight waves 25.6; but 64 rows of
 // 5120 -> 5120, unscaled, with CUs to spare 17.0 and 13.5).  With a
 // scaling and 16 rows what is left is the splitting of x~ in every workgroup, 7.5
-// vector operations a value (13824 -> 5120, fp32 out: 23.4 us, 25.0 on weights that
+// vector operations a value (13824 -> 5120, fp32 out: 24.1 us, 25.0 on weights that
 // come from memory, vector units 74 % busy; 13.8 without).
 template <int NP, int NT, int RT, int NW>
 struct Ring {
@@ -284,11 +284,9 @@ __global__ __launch_bounds__(64 * W, W == 4 ? 2 : 1) void linear_rows_kernel(Lin
   const uint8_t* qw = a.qw + static_cast<size_t>(n0) * (a.K / 2);
   auto copy = [&](int b, int slot) {
     const uint32_t at = ring0 + slot * L::SLOT;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) dma<16>(qw + b * (kBlock / 2), woff[t], at + L::W_OFF + t * 1024);
+    dma_run(qw + b * (kBlock / 2), woff, at + L::W_OFF);
     dma<4>(a.w_scale + static_cast<size_t>((b * kBlock) / a.w_group) * a.N + n0, soff, at + L::S_OFF);
-#pragma unroll
-    for (int i = 0; i < RT * 4; ++i) dma<16>(xs + b * kBlock, xoff[i], at + i * 1024);
+    dma_run(xs + b * kBlock, xoff, at);
     if constexpr (NP > 1) {
       dma<4>(a.dinv + b * kBlock, 4 * lane, at + L::D_OFF);
       dma<4>(a.dinv + b * kBlock + 64, 4 * lane, at + L::D_OFF + 256);
